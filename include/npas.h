@@ -66,6 +66,17 @@
  *     values  per block kept-rows x kept-cols, row major
  *     tiles   per block the same weights as a [Kp/8][Bo][8] tensor-core operand image: element
  *             (c/8, rows[r], c%8) = weight (rows[r], cols[c]); pruned rows and unused columns zero
+ *   Microscaled 4-bit blob (npas_quantize_mx):
+ *     header  32 x uint32: magic 'NPMX' (0x584D504E), version 1, rows, cols, pitch, off_scales,
+ *             off_values (low, high word), total_bytes (low, high word), zeros
+ *     scales  uint8, one per row and 32 columns: 2^(code - 127), 255 = NaN.  In tiles of 128 rows x 4
+ *             blocks (128 columns), 512 bytes each, row tiles major; the scale of (row, block) is byte
+ *             (row%32)*16 + (row%128)/32*4 + block%4 of its tile (the order in which the tensor core
+ *             takes them); rows and blocks past the end 0
+ *     values  rows of pitch = ceil(cols/32)*16 bytes, 4 bits per element (sign, two exponent bits, one
+ *             mantissa bit: 0, 1/2, 1, 3/2, 2, 3, 4, 6 times the scale).  Nibble n of the 32-bit word
+ *             of columns 8j..8j+7 is column 8j + 2n (n < 4) or 8j + 2n - 7 (n >= 4): pairs of columns
+ *             lie 16 bits apart.  Columns past the end 0.
  *   float32 -> bf16 conversion in the packers is round-to-nearest-even on the bit pattern
  *   (bits + 0x7FFF + ((bits >> 16) & 1)) >> 16; a NaN becomes (bits >> 16) | 0x40.
  */
@@ -93,7 +104,8 @@ typedef enum {
     NPAS_ERR_TIMEOUT = 10
 } npas_status;
 
-typedef enum { NPAS_F32 = 0, NPAS_BF16 = 1 } npas_dtype;
+/* (NPAS_MX4: a microscaled 4-bit blob, as the input of npas_linear_mx only) */
+typedef enum { NPAS_F32 = 0, NPAS_BF16 = 1, NPAS_MX4 = 2 } npas_dtype;
 
 /* Bytes of caller workspace every compute call needs (holds the device status words). */
 #define NPAS_WORKSPACE_BYTES 256
@@ -163,6 +175,25 @@ typedef struct {
                         or 8): the form for few output tiles, BN 16 to 128, in which a cluster of KS CTAs shares
                         a tile and splits the input columns; npas_tune_linear_bb measures them */
 } npas_linear_desc;
+
+/* A matrix in microscaled 4-bit floating point: rows of cols columns, blocks of 32 along a row (the last one of a
+ * row may be short); cols up to 2^20.  src_dtype: dtype of the matrix handed to npas_quantize_mx. */
+typedef struct {
+    int32_t rows, cols;
+    int32_t src_dtype; /* npas_dtype */
+} npas_mx_desc;
+
+/* One GEMM call with 4-bit weights.  x_dtype: NPAS_BF16 (rows of I bf16 columns) or NPAS_MX4 (a blob of M rows, I columns);
+ * quantize_x: a bf16 input is quantised on its way in (workspace: npas_linear_mx_workspace), the result is that of
+ * npas_quantize_mx and a call on its blob.  path: 0 = automatic, 1 = force the kernel on CUDA cores (fp32; every
+ * geometry) (NPAS_ERR_UNSUPPORTED when the geometry is outside the requested kernel's envelope). */
+typedef struct {
+    int32_t M, I, O;
+    int32_t x_dtype, quantize_x, y_dtype;
+    int32_t relu, has_bias, has_residual;
+    int32_t path;
+    int32_t variant; /* 0 = the planner's choice */
+} npas_mx_linear_desc;
 
 /* ---- mask helpers (paper Sec. 3: the structural constraint of each scheme) --------------------
  * Derive block masks from a dense 0/1 mask (uint8 per weight, same layout as the weights).
@@ -291,6 +322,32 @@ npas_status npas_linear_bb(const npas_linear_desc *d, const npas_bb_desc *bb, co
                            void *y_dev, void *ws_dev, size_t ws_bytes, void *stream);
 npas_status npas_subsample2d(int32_t N, int32_t H, int32_t W, int32_t C, int32_t stride,
                              int32_t elem_bytes, const void *x_dev, void *y_dev, void *stream);
+
+/* ---- microscaled 4-bit floating point (outside the paper: weights in 4 bits next to weights pruned) ------------
+ * npas_quantize_mx: src [rows][cols] (fp32 or bf16) -> blob of the size npas_quantize_mx_size reports.  A block of
+ *   32 columns of a row with largest magnitude a gets the scale 2^s, s = max(floor(log2 a) - 2, -127) (a = 0: s = -127);
+ *   its elements go to the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 times the scale, ties to the even mantissa, what is past
+ *   6 to 6; signs of zeros are kept.  A block with an infinity or a NaN becomes NaN as a whole.  Zeros stay zeros, so
+ *   what pruning took out stays out.  Bit for bit the same on every call.
+ * npas_dequantize_mx: blob -> the values it stands for, fp32 or bf16 (exact in both).
+ * npas_mx_blob_check: npas_blob_check for these blobs.
+ * npas_linear_mx: GEMM with 4-bit weights (w_blob: O rows, I columns), fused epilogue as in npas_linear_bb
+ *   Y[m,o] = act(bias[o] + sum_i X[m,i] W[o,i] (+ residual[m,o])), sums in fp32, one rounding to y_dtype; any M, I, O
+ *   (O rows of Y and the residual are contiguous).  An infinity or a NaN in a row of X (or a NaN block of W) makes
+ *   what it is multiplied into NaN or infinite; other rows (columns) are untouched; ReLU turns a NaN sum into zero.  y may not alias x or the residual.
+ *   ws_dev: npas_linear_mx_workspace bytes, the first NPAS_WORKSPACE_BYTES zeroed once by the caller before first use (the
+ *   status words); its contents need not survive between calls, and calls that may overlap on the GPU (on two streams, in two
+ *   graphs) need one each.
+ * npas_linear_mx_kernel: id of the kernel the call would run (see path), host only. */
+npas_status npas_quantize_mx_size(const npas_mx_desc *d, size_t *blob_bytes);
+npas_status npas_quantize_mx(const npas_mx_desc *d, const void *src_dev, void *blob_dev, size_t blob_bytes, void *stream);
+npas_status npas_dequantize_mx(const npas_mx_desc *d, const void *blob_dev, size_t blob_bytes, int32_t out_dtype,
+                               void *out_dev, void *stream);
+npas_status npas_mx_blob_check(const npas_mx_desc *d, const void *blob_dev, size_t blob_bytes, void *stream);
+npas_status npas_linear_mx_workspace(const npas_mx_linear_desc *d, size_t *ws_bytes);
+npas_status npas_linear_mx_kernel(const npas_mx_linear_desc *d, int32_t *kernel_id);
+npas_status npas_linear_mx(const npas_mx_linear_desc *d, const void *x_dev, const void *w_blob_dev, const float *bias_dev,
+                           const void *residual_dev, void *y_dev, void *ws_dev, size_t ws_bytes, void *stream);
 
 /* npas_conv2d_bp_static_ws (the paper has no counterpart: this entry exists for callers that must
  * not allocate).  Some callers cannot obtain device memory at the point where they run a layer:

@@ -19,7 +19,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libnpas.so")
 HOST_PATH = os.path.join(_HERE, "_npas_host.so")
 WORKSPACE_BYTES = 256
-F32, BF16 = 0, 1
+F32, BF16, MX4 = 0, 1, 2
 _lib = None
 _host = None                     # the extension module, from the first load() on
 
@@ -48,13 +48,24 @@ class LinearDesc(ctypes.Structure):
                                               "variant")]
 
 
+class MxDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "cols", "src_dtype")]
+
+
+class MxLinearDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("M", "I", "O", "x_dtype", "quantize_x", "y_dtype", "relu", "has_bias", "has_residual", "path",
+                                              "variant")]
+
+
 EXPORTS = ["npas_status_string", "npas_abi_version", "npas_mask_bp_from_dense", "npas_mask_bb_from_dense",
            "npas_pack_bp_size", "npas_pack_bp", "npas_unpack_bp", "npas_pack_bb_size", "npas_pack_bb",
            "npas_unpack_bb", "npas_conv2d_bp", "npas_linear_bb", "npas_blob_check",
            "npas_check_device_status", "npas_launch_count", "npas_maxpool2d", "npas_conv2d_bp_static_ws",
            "npas_subsample2d", "npas_prune_bp_magnitude", "npas_prune_bb_magnitude",
            "npas_conv2d_bp_workspace", "npas_linear_bb_workspace", "npas_conv2d_bp_kernel", "npas_linear_bb_kernel",
-           "npas_tune_conv2d_bp", "npas_tune_linear_bb", "npas_prune_bp_global_workspace", "npas_prune_bp_magnitude_global", "npas_conv2d_bp_maxpool"]
+           "npas_tune_conv2d_bp", "npas_tune_linear_bb", "npas_prune_bp_global_workspace", "npas_prune_bp_magnitude_global", "npas_conv2d_bp_maxpool",
+           "npas_quantize_mx_size", "npas_quantize_mx", "npas_dequantize_mx", "npas_mx_blob_check", "npas_linear_mx_workspace",
+           "npas_linear_mx_kernel", "npas_linear_mx"]
 
 
 def load() -> ctypes.CDLL:
@@ -155,6 +166,12 @@ class BbBlob:
     desc: BbDesc
 
 
+@dataclass
+class MxBlob:
+    data: torch.Tensor          # a matrix in microscaled 4-bit floating point
+    desc: MxDesc
+
+
 def workspace(device="cuda") -> torch.Tensor:
     """Zeroed device scratch for the compute calls (holds the device status words)."""
     return torch.zeros(WORKSPACE_BYTES, dtype=torch.uint8, device=device)
@@ -251,10 +268,30 @@ def mask_bb_from_dense(dense_mask: torch.Tensor, Bo: int, Bi: int):
 
 def blob_check(blob) -> None:
     lib = load()
+    if isinstance(blob, MxBlob):
+        _check(lib.npas_mx_blob_check(ctypes.byref(blob.desc), _p(blob.data), ctypes.c_size_t(blob.data.numel()), _stream()), "npas_mx_blob_check")
+        return
     bp = ctypes.byref(blob.desc) if isinstance(blob, BpBlob) else None
     bb = ctypes.byref(blob.desc) if isinstance(blob, BbBlob) else None
     _check(lib.npas_blob_check(bp, bb, _p(blob.data), ctypes.c_size_t(blob.data.numel()), _stream()),
            "npas_blob_check")
+
+
+def quantize_mx(x: torch.Tensor) -> MxBlob:
+    """npas_quantize_mx: contiguous fp32 or bf16 matrix [rows, cols] -> blob of 4-bit elements with a power-of-two scale for every 32
+    columns of a row (on x's device, on its current stream)."""
+    if _host is None:
+        load()
+    r = _host.quantize_mx(x, MxDesc, MxBlob)
+    return r if type(r) is not int else _refused(r, "npas_quantize_mx")
+
+
+def dequantize_mx(blob: MxBlob, dtype=torch.bfloat16) -> torch.Tensor:
+    """npas_dequantize_mx: the values a blob stands for, [rows, cols] in fp32 or bf16 (exact in both)."""
+    if _host is None:
+        load()
+    r = _host.dequantize_mx(blob.data, blob.desc, dtype)
+    return r if type(r) is not int else _refused(r, "npas_dequantize_mx")
 
 
 # ---------------------------------------------------------------------------- compute ----------
@@ -274,6 +311,21 @@ def linear_bb(x: torch.Tensor, blob: BbBlob, bias=None, residual=None, *, relu=F
         load()
     y = _host.linear_bb(x, blob.data, blob.desc, bias, residual, relu, out_dtype, out, ws, path, variant)
     return y if type(y) is not int else _refused(y, "npas_linear_bb")
+
+
+def linear_mx(x, w: MxBlob, bias=None, residual=None, *, relu=False, out_dtype=None, out=None, quantize_x=False, ws=None, path=0,
+              variant=0) -> torch.Tensor:
+    """npas_linear_mx: x [M, I] times w [O, I] in 4 bits, + bias + residual, ReLU -> [M, O] (bf16 unless ``out_dtype`` says otherwise).
+
+    ``x`` is a bf16 tensor or an MxBlob; with ``quantize_x`` a bf16 tensor is quantised on its way in, as by ``quantize_mx``.  ``ws``: of
+    ``linear_mx_workspace``; without it the call takes scratch memory of its own.  One workspace serves one stream at a time."""
+    if _host is None:
+        load()
+    if isinstance(x, MxBlob):
+        y = _host.linear_mx(x.data, x.desc, w.data, w.desc, bias, residual, relu, out_dtype, out, quantize_x, ws, path, variant)
+    else:
+        y = _host.linear_mx(x, None, w.data, w.desc, bias, residual, relu, out_dtype, out, quantize_x, ws, path, variant)
+    return y if type(y) is not int else _refused(y, "npas_linear_mx")
 
 
 def subsample2d(x: torch.Tensor, stride: int) -> torch.Tensor:
@@ -390,6 +442,35 @@ def linear_bb_kernel(M: int, blob: BbBlob, *, dtype=torch.bfloat16, out_dtype=No
     kid = ctypes.c_int32(0)
     _check(lib.npas_linear_bb_kernel(ctypes.byref(ld), ctypes.byref(d), ctypes.byref(kid)), "npas_linear_bb_kernel")
     return kid.value
+
+
+LINEAR_MX_KERNELS = {1: "linear_mx_simt_kernel"}
+
+
+def _mx_linear_desc(M, w, dtype, out_dtype, quantize_x, relu, bias, residual, path, variant) -> MxLinearDesc:
+    """``dtype``: of the input, a torch dtype or "mx" for an MxBlob."""
+    return MxLinearDesc(int(M), w.desc.cols, w.desc.rows, MX4 if dtype == "mx" else _dt_code(dtype), int(bool(quantize_x)), _dt_code(out_dtype), int(bool(relu)),
+                        int(bool(bias)), int(bool(residual)), int(path), int(variant))
+
+
+def linear_mx_kernel(M: int, w: MxBlob, *, dtype=torch.bfloat16, out_dtype=torch.bfloat16, quantize_x=False, relu=False, bias=False,
+                     residual=False, path=0, variant=0) -> int:
+    """npas_linear_mx_kernel: id of the kernel the call would run (host only; raises NpasError(8) where the path declines)."""
+    d = _mx_linear_desc(M, w, dtype, out_dtype, quantize_x, relu, bias, residual, path, variant)
+    kid = ctypes.c_int32(0)
+    _check(load().npas_linear_mx_kernel(ctypes.byref(d), ctypes.byref(kid)), "npas_linear_mx_kernel")
+    return kid.value
+
+
+def linear_mx_workspace(M: int, w: MxBlob, *, dtype=torch.bfloat16, out_dtype=torch.bfloat16, quantize_x=False, relu=False, bias=False,
+                        residual=False, path=0, variant=0) -> torch.Tensor:
+    """npas_linear_mx_workspace: device scratch for calls of up to these sizes (status words zeroed), on w's device."""
+    d = _mx_linear_desc(M, w, dtype, out_dtype, quantize_x, relu, bias, residual, path, variant)
+    n = ctypes.c_size_t(0)
+    _check(load().npas_linear_mx_workspace(ctypes.byref(d), ctypes.byref(n)), "npas_linear_mx_workspace")
+    ws = torch.empty(n.value, dtype=torch.uint8, device=w.data.device)
+    ws[:WORKSPACE_BYTES].zero_()
+    return ws
 
 
 def tune_conv2d_bp(x: torch.Tensor, blob: BpBlob, bias=None, residual=None, *, stride=1, pad=1, relu=False,

@@ -567,6 +567,142 @@ PyObject *unpack_bb(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- microscaled 4-bit floating point -----------------------------------------------------------------------------
+
+// rows and columns of a 2-D tensor as the descriptors count them
+bool size_arg(const at::Tensor &x, int32_t &rows, int32_t &cols)
+{
+    if (x.size(0) > 0x7FFFFFFF || x.size(1) > 0x7FFFFFFF) return false;
+    rows = (int32_t)x.size(0); cols = (int32_t)x.size(1);
+    return true;
+}
+
+// the bytes of a blob: a contiguous tensor that holds what its descriptor asks for
+bool mx_blob_arg(const at::Tensor &blob, const npas_mx_desc &d, npas_status &s)
+{
+    size_t bytes = 0;
+    s = npas_quantize_mx_size(&d, &bytes);
+    if (s != NPAS_OK) return true;
+    if (!(blob.is_cuda() && blob.is_contiguous() && blob.scalar_type() == at::kByte)) return fail_assert("blob.data must be a contiguous uint8 CUDA tensor");
+    if ((size_t)blob.numel() < bytes) s = NPAS_ERR_BUFFER_TOO_SMALL;
+    return true;
+}
+
+// quantize_mx(x, desc_type, blob_type) -> blob, or the status
+PyObject *quantize_mx(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        const at::Tensor *x;
+        npas_mx_desc d = {};
+        if (n != 3) { PyErr_SetString(PyExc_TypeError, "quantize_mx takes 3 arguments"); return nullptr; }
+        if (!tensor_arg(a[0], x, false, "x")) return nullptr;
+        if (!(x->is_cuda() && x->is_contiguous() && x->dim() == 2)) { fail_assert("x must be a contiguous 2-D CUDA tensor"); return nullptr; }
+        if (!dtype_of(x->scalar_type(), d.src_dtype)) return nullptr;
+        if (!size_arg(*x, d.rows, d.cols)) return PyLong_FromLong(NPAS_ERR_SHAPE);
+        size_t bytes = 0;
+        npas_status s = npas_quantize_mx_size(&d, &bytes);
+        if (s != NPAS_OK) return PyLong_FromLong((long)s);
+        const c10::cuda::CUDAGuard guard(x->device());
+        at::Tensor blob = new_tensor({(int64_t)bytes}, at::kByte, x->device());
+        void *st = c10::cuda::getCurrentCUDAStream().stream();
+        Py_BEGIN_ALLOW_THREADS
+        s = npas_quantize_mx(&d, x->data_ptr(), blob.data_ptr(), bytes, st);
+        Py_END_ALLOW_THREADS
+        return packed(s, std::move(blob), d, a[1], a[2]);
+    });
+}
+
+// dequantize_mx(blob, desc, dtype) -> values, or the status
+PyObject *dequantize_mx(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        const at::Tensor *blob;
+        npas_mx_desc d;
+        at::ScalarType t;
+        int32_t code;
+        npas_status s;
+        if (n != 3) { PyErr_SetString(PyExc_TypeError, "dequantize_mx takes 3 arguments"); return nullptr; }
+        if (!tensor_arg(a[0], blob, false, "blob.data") || !desc_arg(a[1], d) || !dtype_arg(a[2], at::kBFloat16, t) || !dtype_of(t, code)) return nullptr;
+        if (!mx_blob_arg(*blob, d, s)) return nullptr;
+        if (s != NPAS_OK) return PyLong_FromLong((long)s);
+        const c10::cuda::CUDAGuard guard(blob->device());
+        at::Tensor out = new_tensor({d.rows, d.cols}, t, blob->device());
+        void *st = c10::cuda::getCurrentCUDAStream().stream();
+        Py_BEGIN_ALLOW_THREADS
+        s = npas_dequantize_mx(&d, blob->data_ptr(), (size_t)blob->numel(), code, out.data_ptr(), st);
+        Py_END_ALLOW_THREADS
+        return result(s, nullptr, std::move(out));
+    });
+}
+
+// linear_mx(x, x_desc or None, w, w_desc, bias, residual, relu, out_dtype, out, quantize_x, ws, path, variant)
+PyObject *linear_mx(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        const at::Tensor *x, *w, *bias, *res, *out, *ws;
+        npas_mx_desc wd, xd;
+        npas_mx_linear_desc d = {};
+        at::ScalarType ot;
+        npas_status s;
+        if (n != 13) { PyErr_SetString(PyExc_TypeError, "linear_mx takes 13 arguments"); return nullptr; }
+        const bool x_mx = a[1] != Py_None;
+        if (!tensor_arg(a[0], x, false, "x") || (x_mx && !desc_arg(a[1], xd)) || !tensor_arg(a[2], w, false, "w.data") || !desc_arg(a[3], wd) ||
+            !tensor_arg(a[4], bias, true, "bias") || !tensor_arg(a[5], res, true, "residual") || !tensor_arg(a[8], out, true, "out") ||
+            !tensor_arg(a[10], ws, true, "ws") || !int_arg(a[11], d.path) || !int_arg(a[12], d.variant))
+            return nullptr;
+        const int relu = PyObject_IsTrue(a[6]), quantize = PyObject_IsTrue(a[9]);
+        if (relu < 0 || quantize < 0) return nullptr;
+        if (!mx_blob_arg(*w, wd, s)) return nullptr;
+        if (s != NPAS_OK) return PyLong_FromLong((long)s);
+        d.O = wd.rows;
+        if (x_mx) {
+            if (!mx_blob_arg(*x, xd, s)) return nullptr;
+            if (s != NPAS_OK) return PyLong_FromLong((long)s);
+            d.M = xd.rows; d.I = xd.cols; d.x_dtype = NPAS_MX4;
+        } else {
+            if (!(x->is_cuda() && x->is_contiguous() && x->dim() == 2)) { fail_assert("x must be a contiguous 2-D CUDA tensor or an MxBlob"); return nullptr; }
+            if (!dtype_of(x->scalar_type(), d.x_dtype)) return nullptr;
+            if (!size_arg(*x, d.M, d.I)) return PyLong_FromLong(NPAS_ERR_SHAPE);
+        }
+        if (d.I != wd.cols) return PyLong_FromLong(NPAS_ERR_SHAPE);
+        d.relu = relu; d.quantize_x = quantize; d.has_bias = bias != nullptr; d.has_residual = res != nullptr;
+        if (!dtype_arg(a[7], out ? out->scalar_type() : at::kBFloat16, ot) || !dtype_of(ot, d.y_dtype)) return nullptr;
+        const at::Device dev = x->device();
+        auto fits = [&](const at::Tensor *t, at::ScalarType type, at::IntArrayRef size) {
+            return !t || (t->is_cuda() && t->device() == dev && t->is_contiguous() && t->scalar_type() == type && t->sizes() == size);
+        };
+        if (!fits(out, ot, {d.M, d.O})) { fail_assert("out must be a contiguous tensor [rows of x, rows of w] of out_dtype on x's device"); return nullptr; }
+        if (!fits(res, ot, {d.M, d.O})) { fail_assert("residual must be a contiguous tensor of the output's shape and dtype on x's device"); return nullptr; }
+        if (!fits(bias, at::kFloat, {d.O})) { fail_assert("bias must be a contiguous float32 tensor [rows of w] on x's device"); return nullptr; }
+        if (w->device() != dev || (ws && !(ws->is_cuda() && ws->device() == dev && ws->is_contiguous() && ws->scalar_type() == at::kByte))) {
+            fail_assert("w and ws (uint8) must be contiguous on x's device");
+            return nullptr;
+        }
+        size_t need = 0;
+        s = npas_linear_mx_workspace(&d, &need);
+        if (s != NPAS_OK) return PyLong_FromLong((long)s);
+        const c10::cuda::CUDAGuard guard(dev);
+        at::Tensor made, own, scratch;
+        void *status = nullptr, *sp = nullptr;
+        size_t sb = 0;
+        if (!workspace_arg(ws, *x, own, status, sb)) return nullptr;
+        if (ws) {
+            if (sb < need) return PyLong_FromLong(NPAS_ERR_BUFFER_TOO_SMALL);
+            sp = static_cast<uint8_t *>(status) + NPAS_WORKSPACE_BYTES;
+            sb -= NPAS_WORKSPACE_BYTES;
+        } else if ((sb = need - NPAS_WORKSPACE_BYTES) != 0) {
+            scratch = new_tensor({(int64_t)sb}, at::kByte, dev);      // (the stream's: the allocator hands it on in stream order)
+            sp = scratch.data_ptr();
+        }
+        if (!out) made = new_tensor({d.M, d.O}, ot, dev);
+        void *y = out ? out->data_ptr() : made.data_ptr(), *st = c10::cuda::getCurrentCUDAStream().stream();
+        Py_BEGIN_ALLOW_THREADS
+        s = npas_internal_linear_mx(&d, x->data_ptr(), w->data_ptr(), static_cast<const float *>(ptr(bias)), ptr(res), y, status, sp, sb, st);
+        Py_END_ALLOW_THREADS
+        return result(s, out ? a[8] : nullptr, std::move(made));
+    });
+}
+
 // ---- a whole stack of layers --------------------------------------------------------------------------------------
 // One call for the forward pass of a chain of layers: what Python did between the layers (shapes, keys, liveness, two
 // allocations) took longer than the layers of a small batch.  The activations lie in one buffer, placed by first fit over
@@ -845,6 +981,9 @@ PyMethodDef kMethods[] = {
     {"prune_bp_global", (PyCFunction)(void (*)(void))prune_bp_global, METH_FASTCALL, nullptr},
     {"prune_bb", (PyCFunction)(void (*)(void))prune_bb, METH_FASTCALL, nullptr},
     {"unpack_bb", (PyCFunction)(void (*)(void))unpack_bb, METH_FASTCALL, nullptr},
+    {"quantize_mx", (PyCFunction)(void (*)(void))quantize_mx, METH_FASTCALL, nullptr},
+    {"dequantize_mx", (PyCFunction)(void (*)(void))dequantize_mx, METH_FASTCALL, nullptr},
+    {"linear_mx", (PyCFunction)(void (*)(void))linear_mx, METH_FASTCALL, nullptr},
     {"stack_forward", (PyCFunction)(void (*)(void))stack_forward, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 

@@ -51,6 +51,9 @@ npas_status npas_internal_linear_two(const npas_linear_desc *a, const npas_bb_de
 npas_status npas_internal_tune_linear_two(const npas_linear_desc *a, const npas_bb_desc *bba, const npas_linear_desc *b, const npas_bb_desc *bbb,
                                           const void *x, const void *blob1, const float *bias1, const void *residual, void *y1, const void *blob2,
                                           const float *bias2, void *y2, void *ws, size_t ws_bytes, int32_t reps, int32_t *together, float *us, void *stream);
+// npas_linear_mx with its scratch (npas_linear_mx_workspace less the status words) apart from the status words
+npas_status npas_internal_linear_mx(const npas_mx_linear_desc *d, const void *x, const void *w_blob, const float *bias, const void *residual,
+                                    void *y, void *ws, void *scratch, size_t scratch_bytes, void *stream);
 // The plan of the pair convolution (path 7) for a call, as a forced `variant` restricts it: filters per item, position tiles per CTA,
 // rows of a slab, bytes of a slab stage and of a weight stage, stages of each, bytes of shared memory.
 npas_status npas_internal_conv_d2_plan(const npas_conv_desc *d, const npas_bp_desc *bp, int32_t shape[8]);
