@@ -1,6 +1,7 @@
 // Entry points of the GEMM with microscaled 4-bit weights: argument checks, workspace, the choice of a kernel.
 #include "internal_api.h"
 #include "mx.cuh"
+#include "tc_common.cuh"
 
 namespace npas {
 
@@ -19,19 +20,57 @@ npas_status check_args(const npas_mx_linear_desc *d)
     return NPAS_OK;
 }
 
-// 1: CUDA cores.  0: the requested path does not take the geometry.
+// 1: CUDA cores, 3: weights as the 128-row operand.  0: the requested path does not take the geometry.
 int kernel_for(const npas_mx_linear_desc &d)
 {
+    npas_mx_linear_desc in = d;
+    if (in.quantize_x) { in.x_dtype = NPAS_MX4; in.quantize_x = 0; }
     switch (d.path) {
-        case 0: case 1: return 1;
+        case 1: return d.variant ? 0 : 1;
+        case 3: return linear_mx_sw_supported(in) ? 3 : 0;
+        case 0: case 2: break;
+        default: return 0;
     }
-    return 0;
+    if (linear_mx_sw_supported(in)) return 3;
+    return d.path == 2 ? 0 : 1;
 }
 
-// scratch behind the status words: the quantised input
+// Rows of a 16-bit input that do not start on 16-byte boundaries are copied to a pitch that does: the tensor cores' kernels load by TMA.
+bool needs_pitch(const npas_mx_linear_desc &d, int kernel) { return kernel != 1 && d.x_dtype == NPAS_BF16 && !d.quantize_x && d.I % 8 != 0; }
+int64_t pitch_of(const npas_mx_linear_desc &d) { return ((int64_t)d.I + 7) / 8 * 8; }
+
+// scratch behind the status words: the quantised input, or the copied one
 size_t scratch_bytes(const npas_mx_linear_desc &d)
 {
-    return d.quantize_x ? mx_layout(d.M, d.I).total : 0;
+    if (d.quantize_x) return mx_layout(d.M, d.I).total;
+    return needs_pitch(d, kernel_for(d)) ? (size_t)d.M * pitch_of(d) * 2 : 0;
+}
+
+constexpr int kPitchThreads = 256;
+
+// A thread writes 16 bytes of a row; columns past the end are zeros.
+__global__ void __launch_bounds__(kPitchThreads) mx_pitch_kernel(int64_t M, int I, int64_t pieces, const uint16_t *x, uint4 *out)
+{
+    tc::pdl_trigger();
+    tc::pdl_wait();
+    x = tc::behind_wait(x);
+    for (int64_t i = (int64_t)blockIdx.x * kPitchThreads + threadIdx.x; i < M * pieces; i += (int64_t)gridDim.x * kPitchThreads) {
+        const int64_t row = i / pieces;
+        const int c = (int)(i - row * pieces) * 8;
+        uint32_t v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c + j < I ? x[row * I + c + j] : 0u;
+        out[i] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+    }
+}
+
+npas_status pitch_launch(const npas_mx_linear_desc &d, const void *x, void *out, cudaStream_t st)
+{
+    const int64_t pieces = pitch_of(d) / 8, blocks = (d.M * pieces + kPitchThreads - 1) / kPitchThreads, most = (int64_t)sm_count() * 16;
+    const cudaError_t e = tc::launch_pdl(Launch(), mx_pitch_kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(kPitchThreads), 0, st, (int64_t)d.M,
+                                         (int)d.I, pieces, static_cast<const uint16_t *>(x), static_cast<uint4 *>(out));
+    count_launch();
+    return e == cudaSuccess ? launch_status() : NPAS_ERR_CUDA;
 }
 
 }  // namespace
@@ -92,7 +131,18 @@ npas_status npas_internal_linear_mx(const npas_mx_linear_desc *d, const void *x,
         in.x_dtype = NPAS_MX4;
         in.quantize_x = 0;
     }
-    return linear_mx_simt_launch(in, x, w, bias, res, y, st);
+    int64_t pitch = d->I;
+    if (needs_pitch(*d, kernel)) {
+        s = pitch_launch(*d, x, scratch, st);
+        if (s != NPAS_OK) return s;
+        x = scratch;
+        pitch = pitch_of(*d);
+    }
+    switch (kernel) {
+        case 1: return linear_mx_simt_launch(in, x, w, bias, res, y, st);
+        case 3: return linear_mx_sw_launch(in, x, pitch, w, bias, res, y, static_cast<uint32_t *>(ws), st);
+    }
+    return NPAS_ERR_UNSUPPORTED;
 }
 
 }  // extern "C"

@@ -1,0 +1,114 @@
+// tcgen05 wrappers of the kernels on microscaled 4-bit operands: the block-scaled MMA, the copy of scales into tensor memory, the MMA
+// whose first operand lies in tensor memory, stores into it.
+#pragma once
+
+#include "mx.cuh"
+#include "tc_common.cuh"
+
+namespace npas {
+namespace tc {
+
+constexpr uint32_t kMxDescHiSw128 = (1024u >> 4) | (1u << 14) | (2u << 29);      // SBO 1024 bytes, version bit, 128-byte swizzle
+constexpr uint32_t kMxDescLboOne = 1u << 16;                                     // (LBO is not used by swizzled K-major layouts)
+__device__ __forceinline__ uint64_t mx_desc64(uint32_t lo) { return ((uint64_t)kMxDescHiSw128 << 32) | lo; }
+
+// Instruction descriptor: e2m1 x e2m1 -> fp32 with e8m0 scales, both operands K-major, tile M x N, K = 64.  `half`: which two of the
+// four scales in a row's 32-bit word belong to this K step.
+__host__ __device__ constexpr uint32_t idesc_mxf4(uint32_t M, uint32_t N, uint32_t half)
+{
+    return (2u * half << 4) | (1u << 7) | (1u << 10) | ((N >> 3) << 17) | (1u << 23) | ((M >> 4) << 24) | (2u * half << 29);
+}
+
+// D[tmem] (+)= (A[smem] * scales) (B[smem] * scales); issued by ONE thread.
+__device__ __forceinline__ void mma_mxf4_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa_tmem, uint32_t sb_tmem,
+                                            uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa_tmem), "r"(sb_tmem), "r"(accumulate) : "memory");
+}
+
+// D[tmem] (+)= A[tmem: bf16 pairs, 128 lanes x 8 columns] * B[smem]; issued by ONE thread.
+__device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// A tile of scales (512 bytes: 32 rows of 16 bytes) -> four columns of tensor memory, the same in all four lane quarters.  In
+// order with the MMAs that the same thread issues behind it.
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t saddr)
+{
+    const uint64_t desc = smem_desc_kmajor(saddr, 16, 128);
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+
+// 32 consecutive 32-bit columns of the warp's lane quarter (thread i writes TMEM lane base + i).
+__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+          "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+          "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+// Pair i (columns 2i, 2i + 1) of a word of eight elements as bf16 times 2^-126: the magnitude bits are exponent and mantissa.
+template <int i>
+__device__ __forceinline__ uint32_t mx_pair_small(uint32_t w)
+{
+    constexpr int up = 6 - 4 * i;
+    const uint32_t mag = up >= 0 ? w << (up >= 0 ? up : 0) : w >> (up < 0 ? -up : 0);
+    return (mag & 0x01C001C0u) | ((w << (12 - 4 * i)) & 0x80008000u);
+}
+
+// What a block's elements, 2^-126 times their size, are multiplied by to become bf16 values: 2^126 times the scale, in two factors
+// where it is past bf16's range (scales above 2).  Both products are exact.
+struct MxFactor { uint32_t first, second; };
+__device__ __forceinline__ MxFactor mx_factor(uint32_t code)
+{
+    MxFactor f;
+    f.first = (min(code, 128u) + 126u) * 0x00800080u;              // (code 0 to 128: exponents 126 to 254)
+    f.second = code == 255u ? 0x7FC07FC0u : code > 128u ? (code - 1u) * 0x00800080u : 0x3F803F80u;
+    return f;
+}
+
+// ---- host: tensor maps ------------------------------------------------------------------------
+// values of a blob: bytes, boxes of 128 bytes (256 columns) x rows, 128-byte swizzled, past the end zeros
+inline bool mx_encode_values(CUtensorMap *map, const void *blob, const MxLayout &L, int rows, uint32_t box_rows)
+{
+    EncodeTiledFn enc = encode_tiled_fn();
+    if (!enc) return false;
+    const cuuint64_t dims[2] = {L.pitch, (cuuint64_t)rows}, strides[1] = {L.pitch};
+    const cuuint32_t box[2] = {128, box_rows}, estr[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(static_cast<const uint8_t *>(blob)) + L.off_values, dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// a bf16 matrix with rows of `pitch` elements (a multiple of 8): boxes of 64 columns x rows, 128-byte swizzled, past the end zeros
+inline bool mx_encode_bf16(CUtensorMap *map, const void *base, uint64_t cols, uint64_t pitch, uint64_t rows, uint32_t box_rows)
+{
+    EncodeTiledFn enc = encode_tiled_fn();
+    if (!enc) return false;
+    const cuuint64_t dims[2] = {cols, rows}, strides[1] = {pitch * 2};
+    const cuuint32_t box[2] = {64, box_rows}, estr[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace tc
+}  // namespace npas
