@@ -1,0 +1,399 @@
+// GEMM with microscaled 4-bit weights, persistent tiles: 128 outputs x N input rows (N = 128 or 256) per MMA, weights as the
+// 128-row operand like in linear_mx_sw.cu.
+//
+// A CTA per SM walks tiles (outputs fastest, so that the rows of X of a tile are read from L2 by its neighbours).  Copies, MMAs, with a
+// 16-bit input the widening of the weights into tensor memory, and the epilogue are roles of their own that hand stages, slots and
+// accumulators on through barriers, so the next tile is loaded and multiplied while one is written out.  Two accumulators of 128 columns,
+// or one of 256 that the epilogue takes into registers before it does anything else (with 256 rows of X a weight is fetched half as
+// often, which long inputs need).  Tensor memory lane = output: a warp stores 32 consecutive outputs of a row of Y at a time, whatever
+// the alignment of Y's rows, and needs no shared memory for it; residuals are requested before the wait for the accumulator.
+// Every wait is bounded.
+#include <type_traits>
+
+#include "mx_tc.cuh"
+
+namespace npas {
+
+using namespace tc;
+
+namespace {
+
+constexpr int kRows = 128;
+constexpr int kStepCols = 256;                             // columns of a weight stage
+constexpr int kMaxStages = 6, kMaxXStages = 8, kSlots = 4;
+constexpr uint32_t kSmemLimit = 232448;
+constexpr uint32_t kWBytes = kRows * 128;
+constexpr uint32_t kScaleBytes = 2 * kMxScaleTile;         // of 128 rows and a stage
+
+// warps: 0 copies, 1 MMAs, then a 16-bit input's own copies and the widening warps, then the epilogue
+template <bool kMx> struct Roles {
+    static constexpr int kXWarp = 2, kWideWarps = kMx ? 0 : 8, kFirstWide = 3;
+    static constexpr int kFirstEpi = kMx ? 2 : kFirstWide + kWideWarps + 1;          // (a multiple of four behind the 16-bit roles)
+    static constexpr int kEpiWarps = kMx ? 16 : 8;
+    static constexpr int kThreads = (kFirstEpi + kEpiWarps) * 32;
+};
+
+struct MxPsParams {
+    int M, I, O, N, acc, nS, nMT, nOT, n_tiles, nKT, S, SX;    // acc: accumulators; SX: stages of the input (16 bits)
+    int relu, y_bf16;
+    uint32_t x_bytes, xs_bytes, stage_bytes, off_x, off_bar, smem_bytes, tmem_cols, tmem_scales, scale_cols;
+    uint64_t w_scales, x_scales;                           // offsets of the scales in the blobs
+};
+
+struct MxPsBars {
+    uint64_t full[kMaxStages], empty[kMaxStages];
+    uint64_t x_full[kMaxXStages], x_empty[kMaxXStages];
+    uint64_t slot_full[kSlots], slot_empty[kSlots];
+    uint64_t acc_full[2], acc_empty[2];
+    uint32_t tmem_base;
+    uint32_t abort_flag;
+};
+
+// 64 columns of a row: two 16-byte pieces of elements, two scale codes -> 32 pairs of bf16 values
+__device__ __forceinline__ void widen(uint32_t (&r)[32], const uint4 &a, const uint4 &b, uint32_t code0, uint32_t code1)
+{
+    const MxFactor f0 = mx_factor(code0), f1 = mx_factor(code1);
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t f = j < 4 ? f0.first : f1.first;
+        r[4 * j] = mul_bf16x2(mx_pair_small<0>(w[j]), f);
+        r[4 * j + 1] = mul_bf16x2(mx_pair_small<1>(w[j]), f);
+        r[4 * j + 2] = mul_bf16x2(mx_pair_small<2>(w[j]), f);
+        r[4 * j + 3] = mul_bf16x2(mx_pair_small<3>(w[j]), f);
+    }
+    if (__any_sync(0xFFFFFFFFu, code0 > 128u || code1 > 128u)) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) r[j] = mul_bf16x2(r[j], j < 16 ? f0.second : f1.second);
+    }
+}
+
+// 32 rows of one output: bias + residuals, then sums + those, ReLU, one rounding.  `at`: element of the first row; `n`: rows there are
+// (none where the output lies past the end).
+// (The pointer walks from row to row: 32 addresses at once would not fit beside the sums.)
+template <bool kBf16>
+__device__ __forceinline__ void load_residuals(float (&add)[32], float b, const void *res, int64_t at, int64_t O, int n)
+{
+    using T = typename std::conditional<kBf16, uint16_t, float>::type;
+    const T *q = static_cast<const T *>(res) + at;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        add[i] = 0.f;
+        if (i < n) {
+            if constexpr (kBf16) add[i] = __uint_as_float((uint32_t)__ldg(q) << 16);
+            else add[i] = __ldg(q);
+        }
+        q += O;
+        asm volatile("" : "+l"(q));
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) add[i] += b;
+}
+template <bool kBf16>
+__device__ __forceinline__ void store_rows(const uint32_t (&v)[32], float b, void *y, int64_t at, int64_t O, int n, int relu)
+{
+    using T = typename std::conditional<kBf16, uint16_t, float>::type;
+    T *q = static_cast<T *>(y) + at;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        float u = __uint_as_float(v[i]) + b;
+        if (relu) u = fmaxf(u, 0.f);
+        if (i < n) {
+            if constexpr (kBf16) *q = (uint16_t)cvt_bf16x2(u, 0.f);
+            else *q = u;
+        }
+        q += O;
+        asm volatile("" : "+l"(q));
+    }
+}
+
+template <bool kMx, bool kBf16>
+__global__ void __launch_bounds__(Roles<kMx>::kThreads, 1)
+linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w, const MxPsParams p, const uint8_t *xblob,
+                    const uint8_t *wblob, const float *bias, const void *res, void *y, uint32_t *ws)
+{
+    using R = Roles<kMx>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    MxPsBars *bars = reinterpret_cast<MxPsBars *>(smem + p.off_bar);
+    volatile uint32_t *abort_flag = &bars->abort_flag;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int nK = (p.I + 63) / 64;                        // K steps of 64 columns
+
+    if (tid == 0) {
+        for (int s = 0; s < p.S; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], kMx ? 1 : R::kWideWarps); }
+        for (int s = 0; s < p.SX; ++s) { mbar_init(&bars->x_full[s], 1); mbar_init(&bars->x_empty[s], 1); }
+        for (int s = 0; s < kSlots; ++s) { mbar_init(&bars->slot_full[s], 4); mbar_init(&bars->slot_empty[s], 1); }
+        for (int a = 0; a < 2; ++a) { mbar_init(&bars->acc_full[a], 1); mbar_init(&bars->acc_empty[a], R::kEpiWarps); }
+        bars->abort_flag = 0;
+        fence_barrier_init();
+        prefetch_tensormap(&tmap_x);
+        prefetch_tensormap(&tmap_w);
+    }
+    if (warp == 1) tmem_alloc(&bars->tmem_base, p.tmem_cols);
+    pdl_trigger();
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem_base = bars->tmem_base;
+    pdl_wait();
+    const int z = zero_behind_wait();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t s = 0, lap = 0;
+            bool ok = true;
+            for (int tile = blockIdx.x; tile < p.n_tiles && ok; tile += gridDim.x) {
+                const int mt = tile / p.nOT, ot = tile - mt * p.nOT;
+                for (int step = 0; step < p.nS; ++step) {
+                    if (lap >= 1 && !mbar_wait(&bars->empty[s], (lap & 1u) ^ 1u, abort_flag, ws, 0xB100)) { ok = false; break; }
+                    uint8_t *st = smem + (size_t)s * p.stage_bytes;
+                    const uint32_t sb = (uint32_t)min(2, p.nKT - 2 * step) * kMxScaleTile;   // (the last tile of columns may stand alone)
+                    // row tiles of X's scales: those that exist
+                    const int xt = kMx ? min(p.N / kRows, (p.M + kRows - 1) / kRows - mt * (p.N / kRows)) : 0;
+                    mbar_arrive_expect_tx(&bars->full[s], kWBytes + sb + (kMx ? p.x_bytes + xt * sb : 0u));
+                    tma_load_2d(st, &tmap_w, &bars->full[s], step * 128, ot * kRows);
+                    bulk_load_1d(st + kWBytes, wblob + p.w_scales + ((uint64_t)ot * p.nKT + 2 * step) * kMxScaleTile, sb, &bars->full[s]);
+                    if (kMx) {
+                        tma_load_2d(st + kWBytes + kScaleBytes + p.xs_bytes, &tmap_x, &bars->full[s], step * 128, mt * p.N);
+                        for (int t = 0; t < xt; ++t)
+                            bulk_load_1d(st + kWBytes + kScaleBytes + t * kScaleBytes,
+                                         xblob + p.x_scales + ((uint64_t)(mt * (p.N / kRows) + t) * p.nKT + 2 * step) * kMxScaleTile, sb, &bars->full[s]);
+                    }
+                    if (++s == (uint32_t)p.S) { s = 0; ++lap; }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (elect_one()) {
+            const uint32_t base = smem_u32(smem) & 0x3FFFFu;
+            uint32_t s = 0, ph = 0, it = 0, k_all = 0;
+            bool ok = true;
+            for (int tile = blockIdx.x; tile < p.n_tiles && ok; tile += gridDim.x, ++it) {
+                const uint32_t acc = p.acc == 2 ? it & 1u : 0u, lap_acc = p.acc == 2 ? it >> 1 : it;
+                if (lap_acc >= 1 && !mbar_wait(&bars->acc_empty[acc], (lap_acc & 1u) ^ 1u, abort_flag, ws, 0xB200)) break;
+                tc_fence_after_sync();
+                const uint32_t d_tmem = tmem_base + acc * p.N;
+                if (kMx) {
+                    for (int step = 0; step < p.nS; ++step) {
+                        if (!mbar_wait(&bars->full[s], ph, abort_flag, ws, 0xB300)) { ok = false; break; }
+                        tc_fence_after_sync();
+                        const uint32_t st = base + s * p.stage_bytes, a_lo = (st >> 4) | kMxDescLboOne;
+                        const uint32_t b_lo = ((st + kWBytes + kScaleBytes + p.xs_bytes) >> 4) | kMxDescLboOne;
+                        // tensor memory of this stage's scales: two tiles of W's, then X's, a K tile's row tiles side by side
+                        const uint32_t sf = tmem_base + p.tmem_scales + s * p.scale_cols, xc = (uint32_t)p.N / 32;
+                        const int n = min(4, nK - 4 * step);
+                        for (int t = 0; t < (n + 1) / 2; ++t) {
+                            copy_scales(sf + 4 * t, st + kWBytes + t * kMxScaleTile);
+                            for (int r = 0; r < p.N / kRows; ++r)
+                                copy_scales(sf + 8 + xc * t + 4 * r, st + kWBytes + kScaleBytes + r * kScaleBytes + t * kMxScaleTile);
+                        }
+                        for (int j = 0; j < n; ++j)                                  // 64 columns = 32 bytes inside the swizzled row
+                            mma_mxf4_ss(d_tmem, mx_desc64(a_lo + 2 * j), mx_desc64(b_lo + 2 * j), idesc_mxf4(128, (uint32_t)p.N, j & 1),
+                                        sf + 4 * (j / 2), sf + 8 + xc * (j / 2), step > 0 || j > 0);
+                        mma_commit(&bars->empty[s]);
+                        if (++s == (uint32_t)p.S) { s = 0; ph ^= 1u; }
+                    }
+                } else {
+                    const uint32_t idesc = idesc_bf16_f32(128, (uint32_t)p.N), xb = base + p.off_x;
+                    for (int k = 0; k < nK; ++k, ++k_all) {
+                        const uint32_t slot = k_all % kSlots;
+                        if (!mbar_wait(&bars->x_full[s], ph, abort_flag, ws, 0xB310) ||
+                            !mbar_wait(&bars->slot_full[slot], (k_all / kSlots) & 1u, abort_flag, ws, 0xB320)) { ok = false; break; }
+                        tc_fence_after_sync();
+                        const uint32_t b_lo = ((xb + s * p.x_bytes) >> 4) | kMxDescLboOne, a_t = tmem_base + p.tmem_scales + slot * 32u;
+#pragma unroll
+                        for (uint32_t j = 0; j < 4; ++j)
+                            mma_bf16_ts(d_tmem, a_t + 8 * j, mx_desc64(b_lo + 2 * j), idesc, (k > 0 || j > 0) ? 1u : 0u);
+                        mma_commit(&bars->slot_empty[slot]);
+                        mma_commit(&bars->x_empty[s]);
+                        if (++s == (uint32_t)p.SX) { s = 0; ph ^= 1u; }
+                    }
+                }
+                if (ok) mma_commit(&bars->acc_full[acc]);
+            }
+        }
+    } else if (!kMx && warp == R::kXWarp) {
+        if (lane == 0) {
+            uint32_t s = 0, lap = 0;
+            bool ok = true;
+            for (int tile = blockIdx.x; tile < p.n_tiles && ok; tile += gridDim.x) {
+                const int mt = tile / p.nOT;
+                for (int k = 0; k < nK; ++k) {
+                    if (lap >= 1 && !mbar_wait(&bars->x_empty[s], (lap & 1u) ^ 1u, abort_flag, ws, 0xB110)) { ok = false; break; }
+                    mbar_arrive_expect_tx(&bars->x_full[s], p.x_bytes);
+                    tma_load_2d(smem + p.off_x + (size_t)s * p.x_bytes, &tmap_x, &bars->x_full[s], k * 64, mt * p.N);
+                    if (++s == (uint32_t)p.SX) { s = 0; ++lap; }
+                }
+            }
+        }
+    } else if (!kMx && warp < R::kFirstWide + R::kWideWarps) {
+        // ---- widening: group g of four warps takes every second K step, a thread one row of the weights -----------------
+        const int group = (warp - R::kFirstWide) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+        bool ok = true;
+        uint32_t s = 0, ph = 0, k0 = 0;                        // k0: K steps before this stage
+        for (int tile = blockIdx.x; tile < p.n_tiles && ok; tile += gridDim.x) {
+            for (int step = 0; step < p.nS && ok; ++step) {
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->full[s], ph, abort_flag, ws, 0xB400));
+                if (!ok) break;
+                const uint8_t *st = smem + (size_t)s * p.stage_bytes;
+                const int n = min(4, nK - 4 * step);
+                for (int q = (int)((group ^ k0) & 1u); q < n; q += 2) {
+                    const uint32_t k = k0 + q, slot = k % kSlots;
+                    const uint4 a = *reinterpret_cast<const uint4 *>(st + r * 128 + ((2 * q) ^ (r & 7)) * 16);
+                    const uint4 b = *reinterpret_cast<const uint4 *>(st + r * 128 + ((2 * q + 1) ^ (r & 7)) * 16);
+                    const uint32_t codes = *reinterpret_cast<const uint32_t *>(st + kWBytes + (q >> 1) * kMxScaleTile + lane * 16 + quarter * 4) >> (16 * (q & 1));
+                    uint32_t v[32];
+                    widen(v, a, b, codes & 255u, (codes >> 8) & 255u);
+                    if (k >= kSlots) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->slot_empty[slot], ((k / kSlots) & 1u) ^ 1u, abort_flag, ws, 0xB410));
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    tmem_st_x32(tmem_base + ((uint32_t)(quarter * 32) << 16) + p.tmem_scales + slot * 32u, v);
+                    tmem_st_wait();
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bars->slot_full[slot]);
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars->empty[s]);
+                k0 += n;
+                if (++s == (uint32_t)p.S) { s = 0; ph ^= 1u; }
+            }
+        }
+    } else if (warp >= R::kFirstEpi) {
+        // ---- epilogue: warp -> lane quarter and a share of the accumulator's columns -------------------------------------
+        const int quarter = warp & 3, part = (warp - R::kFirstEpi) >> 2, share = p.N / (R::kEpiWarps / 4);
+        uint32_t it = 0;
+        for (int tile = blockIdx.x; tile < p.n_tiles; tile += gridDim.x, ++it) {
+            const int mt = tile / p.nOT, ot = tile - mt * p.nOT, o = ot * kRows + quarter * 32 + lane;
+            const uint32_t acc = p.acc == 2 ? it & 1u : 0u, lap = p.acc == 2 ? it >> 1 : it;
+            const int m0 = mt * p.N + part * share;
+            const int64_t at = (int64_t)m0 * p.O + o + z;
+            const int n = o < p.O ? p.M - m0 : 0;              // rows from m0 on (may be none)
+            const uint32_t t_addr = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * p.N + (uint32_t)(part * share);
+            const float b = bias && o < p.O ? __ldg(bias + o + z) : 0.f;
+            // the accumulator is in registers: the MMA warp may overwrite it
+            auto release = [&]() {
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars->acc_empty[acc]);
+            };
+            uint32_t v[32];
+            if (kMx && p.acc == 1 && !res) {
+                // one accumulator: both batches of the share at once (the residuals' registers are free)
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&bars->acc_full[acc], lap & 1u, abort_flag, ws, 0xB500))) break;
+                tc_fence_after_sync();
+                uint32_t v2[32];
+                tmem_ld_x32(t_addr, v);
+                tmem_ld_x32(t_addr + 32, v2);
+                tmem_ld_wait();
+                release();
+                store_rows<kBf16>(v, b, y, at, p.O, n, p.relu);
+                store_rows<kBf16>(v2, b, y, at + (int64_t)32 * p.O, p.O, n - 32, p.relu);
+                continue;
+            }
+            float add[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) add[i] = b;
+            if (res) load_residuals<kBf16>(add, b, res, at, p.O, n);
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait(&bars->acc_full[acc], lap & 1u, abort_flag, ws, 0xB510))) break;
+            tc_fence_after_sync();
+            for (int c = 0; c < share; c += 32) {
+                tmem_ld_x32(t_addr + c, v);
+                tmem_ld_wait();
+                if (c + 32 == share) release();
+                if (c && res) load_residuals<kBf16>(add, b, res, at + (int64_t)c * p.O, p.O, n - c);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + add[i]);
+                store_rows<kBf16>(v, 0.f, y, at + (int64_t)c * p.O, p.O, n - c, p.relu);
+            }
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (*abort_flag) {
+        // a role gave up: leave time for copies still in flight to land before the CTA retires
+        const long long t0 = clock64();
+        while (clock64() - t0 < 400000ll) { }
+        __syncthreads();
+    }
+    if (warp == 1) {
+        tc_fence_after_sync();
+        tmem_dealloc(tmem_base, p.tmem_cols);
+    }
+}
+
+bool plan(const npas_mx_linear_desc &d, MxPsParams &p, int sms)
+{
+    const bool mx = d.x_dtype == NPAS_MX4;
+    const MxLayout LW = mx_layout(d.O, d.I), LX = mx_layout(d.M, d.I);
+    p = MxPsParams{};
+    p.M = d.M; p.I = d.I; p.O = d.O;
+    p.relu = d.relu; p.y_bf16 = d.y_dtype == NPAS_BF16;
+    p.nS = (d.I + kStepCols - 1) / kStepCols;
+    p.nKT = (int)LW.nKT;
+    p.nOT = (d.O + kRows - 1) / kRows;
+    p.N = d.variant ? d.variant : (d.I >= 2048 && (long long)((d.M + 255) / 256) * p.nOT >= sms ? 256 : 128);
+    if (p.N != 128 && p.N != 256) return false;
+    p.acc = p.N == 128 ? 2 : 1;
+    p.nMT = (d.M + p.N - 1) / p.N;
+    const long long tiles = (long long)p.nMT * p.nOT;
+    if (tiles > 0x7FFFFFFF) return false;
+    p.n_tiles = (int)tiles;
+    p.w_scales = LW.off_scales; p.x_scales = LX.off_scales;
+    p.x_bytes = (uint32_t)p.N * 128u;
+    p.xs_bytes = mx ? (uint32_t)p.N / kRows * kScaleBytes : 0u;
+    p.stage_bytes = round_up(kWBytes + kScaleBytes + (mx ? p.xs_bytes + p.x_bytes : 0u), 1024);
+    const uint32_t budget = kSmemLimit - (uint32_t)sizeof(MxPsBars) - 128u - 1024u;
+    if (!mx) p.SX = p.N == 256 ? 4 : 8;
+    p.S = (int)((budget - (uint32_t)p.SX * p.x_bytes) / p.stage_bytes);
+    if (p.S > kMaxStages) p.S = kMaxStages;
+    if (p.S < 2) return false;
+    p.off_x = (uint32_t)p.S * p.stage_bytes;
+    p.off_bar = round_up(p.off_x + (uint32_t)p.SX * p.x_bytes, 128);
+    p.smem_bytes = p.off_bar + (uint32_t)sizeof(MxPsBars) + 1024u;
+    if (p.smem_bytes > kSmemLimit) return false;
+    p.tmem_scales = 256;
+    p.scale_cols = 8 + 2 * (uint32_t)p.N / 32;
+    const uint32_t cols = p.tmem_scales + (mx ? p.scale_cols * p.S : 32u * kSlots);
+    p.tmem_cols = 32;
+    while (p.tmem_cols < cols) p.tmem_cols *= 2;
+    return p.tmem_cols <= 512;
+}
+
+bool planned(const npas_mx_linear_desc &d, MxPsParams &p)
+{
+    const int32_t none = 0;
+    return cached_plan(d, none, 0, p, [&](MxPsParams &q) { return plan(d, q, sm_count()); });
+}
+
+}  // namespace
+
+bool linear_mx_ps_supported(const npas_mx_linear_desc &d)
+{
+    MxPsParams p;
+    return planned(d, p);
+}
+
+npas_status linear_mx_ps_launch(const npas_mx_linear_desc &d, const void *x, int64_t x_pitch, const void *w, const float *bias, const void *res, void *y,
+                                uint32_t *ws, cudaStream_t st)
+{
+    MxPsParams p;
+    if (!planned(d, p)) return NPAS_ERR_UNSUPPORTED;
+    const bool mx = d.x_dtype == NPAS_MX4;
+    CUtensorMap tmx, tmw;
+    if (!mx_encode_values(&tmw, w, mx_layout(d.O, d.I), d.O, kRows)) return NPAS_ERR_CUDA;
+    if (!(mx ? mx_encode_values(&tmx, x, mx_layout(d.M, d.I), d.M, (uint32_t)p.N)
+             : mx_encode_bf16(&tmx, x, (uint64_t)d.I, (uint64_t)x_pitch, (uint64_t)d.M, (uint32_t)p.N)))
+        return NPAS_ERR_CUDA;
+    const auto kernel = mx ? (p.y_bf16 ? linear_mx_ps_kernel<true, true> : linear_mx_ps_kernel<true, false>)
+                           : (p.y_bf16 ? linear_mx_ps_kernel<false, true> : linear_mx_ps_kernel<false, false>);
+    if (allow_dynamic_smem(reinterpret_cast<const void *>(kernel), (int)kSmemLimit) != NPAS_OK) return NPAS_ERR_CUDA;
+    const int sms = sm_count();
+    const cudaError_t e = launch_pdl(Launch(), kernel, dim3((unsigned)(p.n_tiles < sms ? p.n_tiles : sms)), dim3(mx ? Roles<true>::kThreads : Roles<false>::kThreads),
+                                     p.smem_bytes, st, tmx, tmw, p, static_cast<const uint8_t *>(x), static_cast<const uint8_t *>(w), bias, res, y, ws);
+    count_launch();
+    return e == cudaSuccess ? launch_status() : NPAS_ERR_CUDA;
+}
+
+}  // namespace npas
