@@ -8,17 +8,16 @@
 // What bounds both directions: bytes (2.53 per bf16 element, 4.53 per fp32 one).  A block of threads takes 128 rows x 128 columns,
 // which is one 512-byte tile of scales: 16 lanes share a row with eight columns each (one 16-byte load of bf16, one word of
 // nibbles stored), a block's maximum crosses four lanes, eight rows' loads of a thread are in flight together, and the tile of scales
-// is put together in shared memory and leaves in whole sectors.
-#include "mx.cuh"
-#include "tc_common.cuh"
+// is put together in shared memory and leaves in whole sectors.  Maxima and scaling on pairs of bf16: with every element as a float
+// 125 instructions for eight of them bound it (200704x256 57 us, now 21: 94 % of the copy rate; fp32 36.7, 97 %; back 22.3 and
+// 38.6).
+#include "mx_tc.cuh"
 
 namespace npas {
 
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRowsPerPass = kThreads / 16;
-constexpr int kPasses = kMxTileRows / kRowsPerPass;
 
 // Eight floats -> a word of e2m1 elements in the order of mx_nibble: to nearest even, past 6 to 6.
 __device__ __forceinline__ uint32_t cvt_e2m1x8(const float (&v)[8])
@@ -34,78 +33,122 @@ __device__ __forceinline__ uint32_t cvt_e2m1x8(const float (&v)[8])
     return d;
 }
 
-// Eight columns of a row as floats, zeros past the end.  `whole`: rows start on 16-byte boundaries and 8 divides the columns.
-template <typename T>
-__device__ __forceinline__ void load8(float (&v)[8], const T *row, int c, int cols, bool whole)
+// Eight columns of a row as they are, zeros past the end (bf16 in pairs: four words; fp32: eight).  `whole`: rows start on 16-byte
+// boundaries and 8 divides the columns.
+template <int W>
+__device__ __forceinline__ void load8(uint32_t (&v)[W], const void *row, int c, int cols, bool whole)
 {
-    if (whole) {
-        if constexpr (sizeof(T) == 2) {
-            uint4 u = make_uint4(0, 0, 0, 0);
-            if (c < cols) u = *reinterpret_cast<const uint4 *>(row + c);
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    constexpr bool kHalf = W == 4;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+    for (int i = 0; i < W; ++i) v[i] = 0u;
+    if (whole) {
+        if (c >= cols) return;
+        if constexpr (kHalf) {
+            const uint4 u = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(row) + c);
+            v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
         } else {
-            float4 a = make_float4(0, 0, 0, 0), b = a;
-            if (c < cols) { a = *reinterpret_cast<const float4 *>(row + c); b = *reinterpret_cast<const float4 *>(row + c + 4); }
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+            tc::ld_sector(v, static_cast<const uint32_t *>(row) + c);
         }
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if constexpr (sizeof(T) == 2) v[i] = c + i < cols ? bf16_bits_to_f32(row[c + i]) : 0.f;
-        else v[i] = c + i < cols ? row[c + i] : 0.f;
+    for (int i = 0; i < 8; ++i)
+        if (c + i < cols) {
+            if constexpr (kHalf) v[i / 2] |= (uint32_t)static_cast<const uint16_t *>(row)[c + i] << (16 * (i & 1));
+            else v[i] = static_cast<const uint32_t *>(row)[c + i];
+        }
+}
+
+// largest magnitude of the eight, the upper half of its bits (infinities and NaN come out above every number)
+template <int W>
+__device__ __forceinline__ uint32_t top8(const uint32_t (&v)[W])
+{
+    if constexpr (W == 4) {
+        uint32_t m = __vmaxu2(__vmaxu2(v[0] & 0x7FFF7FFFu, v[1] & 0x7FFF7FFFu), __vmaxu2(v[2] & 0x7FFF7FFFu, v[3] & 0x7FFF7FFFu));
+        return max(m & 0xFFFFu, m >> 16);
+    } else {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, v[i] & 0x7FFFFFFFu);
+        return m >> 16;
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) quantize_mx_kernel(int rows, int cols, int whole, const T *src, uint8_t *blob)
+// the eight times 2^(127 - code), as floats.  (In pairs of bf16 where they are: what falls below bf16's smallest number is far below 1/4.)
+template <int W>
+__device__ __forceinline__ void scaled8(float (&f)[8], const uint32_t (&v)[W], uint32_t code)
 {
-    __shared__ uint32_t scales[kMxTileRows];            // word (r % 32) * 4 + r / 32: the four codes of row r
+    const uint32_t e = 254u - min(code, 253u);                 // (the NaN block's elements mean nothing)
+    if constexpr (W == 4) {
+        const uint32_t inv = e * 0x00800080u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t u = tc::mul_bf16x2(v[i], inv);
+            f[2 * i] = __uint_as_float(u << 16);
+            f[2 * i + 1] = __uint_as_float(u & 0xFFFF0000u);
+        }
+    } else {
+        const float inv = __uint_as_float(e << 23);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[i]) * inv;
+    }
+}
+
+template <typename T, bool kParts, int kLanes>
+__global__ void __launch_bounds__(kThreads) quantize_mx_kernel(int rows, int cols, int whole, int n_parts, const T *src, uint8_t *blob)
+{
+    __shared__ __align__(16) uint8_t scales[kMxScaleTile];
     const MxLayout L = mx_layout(rows, cols);
-    const uint32_t rt = blockIdx.x / L.nKT, kt = blockIdx.x - rt * L.nKT;
-    const int lane16 = threadIdx.x & 15, r0 = threadIdx.x >> 4, c = (int)(kt * kMxTileCols) + lane16 * 8;
+    constexpr int kRowsPerPass = kThreads / kLanes, kPasses = kMxTileRows / kRowsPerPass;
+    const int parts = kParts ? n_parts : 1;
+    const uint32_t tile = blockIdx.x / parts, part = blockIdx.x - tile * parts, rt = tile / L.nKT, kt = tile - rt * L.nKT;
+    const int rows_part = kMxTileRows / parts, row_lo = (int)part * rows_part;   // this block's rows of the tile
+    const int lane = threadIdx.x % kLanes, r0 = row_lo + threadIdx.x / kLanes, c = (int)(kt * kMxTileCols) + lane * 8;
+    const int rows_here = min(rows - (int)(rt * kMxTileRows) - row_lo, rows_part), left = rows_here + row_lo - r0;   // pass p has a row where p * kRowsPerPass < left
     tc::pdl_trigger();
     tc::pdl_wait();
     src = tc::behind_wait(src);
     blob = tc::behind_wait(blob);
     uint8_t *values = blob + L.off_values;
-    const bool stored = (uint32_t)c < 2 * L.pitch;
-    float v[kPasses][8];
-#pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-        const int64_t row = (int64_t)rt * kMxTileRows + p * kRowsPerPass + r0;
-        if (row < rows) load8(v[p], src + row * cols, c, cols, whole);
-        else
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[p][i] = 0.f;
+    // passes that have rows (a tile of few rows is latency: one row of 2048 columns took 2.2 us with all eight)
+    const int passes = (max(rows_here, 0) + kRowsPerPass - 1) / kRowsPerPass;
+    if (kLanes < 16 || passes < kPasses) {
+        if (threadIdx.x < kMxTileRows) reinterpret_cast<uint32_t *>(scales)[threadIdx.x] = 0u;
+        __syncthreads();
     }
+    constexpr int W = sizeof(T) == 2 ? 4 : 8;
+    uint32_t v[kPasses][W];
+    const int64_t row0 = (int64_t)rt * kMxTileRows + r0;
+    const T *from = src + row0 * cols;
 #pragma unroll
     for (int p = 0; p < kPasses; ++p) {
-        const int r = p * kRowsPerPass + r0;
-        const int64_t row = (int64_t)rt * kMxTileRows + r;
-        // largest magnitude as a bit pattern: infinities and NaN come out above every number
-        uint32_t top = 0;
+        if (p >= passes) break;
+        load8(v[p], from, p * kRowsPerPass < left ? c : cols, cols, whole);
+        from += (int64_t)kRowsPerPass * cols;
+    }
+    uint8_t *to = values + (uint64_t)row0 * L.pitch + c / 2;
+    const bool stored = (uint32_t)c < 2 * L.pitch;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[p][i]) & 0x7FFFFFFFu);
+    for (int p = 0; p < kPasses; ++p) {
+        if (p >= passes) break;
+        const int r = p * kRowsPerPass + r0;
+        uint32_t top = top8(v[p]);
         top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
         top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-        const uint32_t e = top >> 23, code = e == 255 ? 255u : e > 2 ? e - 2 : 0u;
-        const float inv = __uint_as_float((254u - min(code, 253u)) << 23);       // 2^(127 - code); the NaN block's elements mean nothing
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[p][i] *= inv;
-        const uint32_t word = code == 255 ? 0u : cvt_e2m1x8(v[p]);
-        if (row < rows && stored) *reinterpret_cast<uint32_t *>(values + (uint64_t)row * L.pitch + c / 2) = word;
-        uint32_t codes = row < rows && c < cols ? code << (8 * (lane16 >> 2)) : 0u;
-        // (a short last block has lanes past the end that must not hide its code)
-        codes |= __shfl_xor_sync(0xFFFFFFFFu, codes, 1); codes |= __shfl_xor_sync(0xFFFFFFFFu, codes, 2);
-        codes |= __shfl_xor_sync(0xFFFFFFFFu, codes, 4); codes |= __shfl_xor_sync(0xFFFFFFFFu, codes, 8);
-        if (lane16 == 0) scales[(r & 31) * 4 + (r >> 5)] = codes;
+        const uint32_t e = top >> 7, code = e == 255 ? 255u : e > 2 ? e - 2 : 0u;
+        float f[8];
+        scaled8(f, v[p], code);
+        const uint32_t word = cvt_e2m1x8(f);
+        if (p * kRowsPerPass < left && stored) *reinterpret_cast<uint32_t *>(to) = code == 255 ? 0u : word;
+        to += (uint64_t)kRowsPerPass * L.pitch;
+        if ((lane & 3) == 0) scales[mx_scale_at((uint32_t)r, (uint32_t)lane >> 2)] = (uint8_t)code;   // (rows and blocks past the end: 0)
     }
     __syncthreads();
-    if (threadIdx.x < kMxTileRows)
-        reinterpret_cast<uint32_t *>(blob + L.off_scales + (uint64_t)blockIdx.x * kMxScaleTile)[threadIdx.x] = scales[threadIdx.x];
+    if ((int)threadIdx.x < rows_part) {
+        // the whole tile in order, or the words of this block's rows
+        const int r = row_lo + (int)threadIdx.x, word = parts == 1 ? (int)threadIdx.x : (r & 31) * 4 + (r >> 5);
+        reinterpret_cast<uint32_t *>(blob + L.off_scales + (uint64_t)tile * kMxScaleTile)[word] = reinterpret_cast<const uint32_t *>(scales)[word];
+    }
     // header, and the padding behind the last row
     if (blockIdx.x == 0 && threadIdx.x < 32) {
         uint32_t h = 0;
@@ -128,74 +171,115 @@ __global__ void __launch_bounds__(kThreads) quantize_mx_kernel(int rows, int col
 }
 
 template <typename T>
-__device__ __forceinline__ void store8(T *row, int c, int cols, bool whole, const float (&v)[8])
+__device__ __forceinline__ void store8(T *row, int c, const float (&v)[8])
 {
-    if (whole) {
-        if (c >= cols) return;
         if constexpr (sizeof(T) == 2) {
             *reinterpret_cast<uint4 *>(row + c) = make_uint4(tc::cvt_bf16x2(v[0], v[1]), tc::cvt_bf16x2(v[2], v[3]), tc::cvt_bf16x2(v[4], v[5]),
                                                              tc::cvt_bf16x2(v[6], v[7]));
         } else {
-            *reinterpret_cast<float4 *>(row + c) = make_float4(v[0], v[1], v[2], v[3]);
-            *reinterpret_cast<float4 *>(row + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
-        }
-        return;
-    }
+            uint32_t o[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (c + i < cols) {
-            if constexpr (sizeof(T) == 2) row[c + i] = (uint16_t)tc::cvt_bf16x2(v[i], 0.f);
-            else row[c + i] = v[i];
+            for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(v[i]);
+            tc::st_sector(row + c, o);
         }
 }
 
 // (element times 2^126, then times the scale: both exact; every value is a bf16 number too, subnormals included)
-template <typename T>
-__global__ void __launch_bounds__(kThreads) dequantize_mx_kernel(int rows, int cols, int whole, const uint8_t *blob, T *out)
+template <typename T, bool kParts, int kLanes>
+__global__ void __launch_bounds__(kThreads) dequantize_mx_kernel(int rows, int cols, int whole, int n_parts, const uint8_t *blob, T *out)
 {
     const MxLayout L = mx_layout(rows, cols);
-    const uint32_t rt = blockIdx.x / L.nKT, kt = blockIdx.x - rt * L.nKT;
-    const int lane16 = threadIdx.x & 15, r0 = threadIdx.x >> 4, c = (int)(kt * kMxTileCols) + lane16 * 8;
+    constexpr int kRowsPerPass = kThreads / kLanes, kPasses = kMxTileRows / kRowsPerPass;
+    const int parts = kParts ? n_parts : 1;
+    const uint32_t tile = blockIdx.x / parts, part = blockIdx.x - tile * parts, rt = tile / L.nKT, kt = tile - rt * L.nKT;
+    const int rows_part = kMxTileRows / parts, row_lo = (int)part * rows_part;
+    const int lane = threadIdx.x % kLanes, r0 = row_lo + threadIdx.x / kLanes;
     tc::pdl_trigger();
     tc::pdl_wait();
     blob = tc::behind_wait(blob);
     out = tc::behind_wait(out);
-    if (c >= cols) return;
-    const uint8_t *scales = blob + L.off_scales + (uint64_t)blockIdx.x * kMxScaleTile, *values = blob + L.off_values;
-    uint32_t word[kPasses], code[kPasses];
+    const uint8_t *scales = blob + L.off_scales + (uint64_t)tile * kMxScaleTile;
+    const int64_t row0 = (int64_t)rt * kMxTileRows + r0;
+    const uint8_t *from = blob + L.off_values + (uint64_t)row0 * L.pitch + kt * (kMxTileCols / 2);
+    T *to = out + row0 * cols + kt * kMxTileCols;
+    const int left = min(rows - (int)(rt * kMxTileRows), row_lo + rows_part) - r0, width = cols - (int)(kt * kMxTileCols);
+    if (whole) {
+        if (lane * 8 >= width) return;
+        uint32_t word[kPasses], code[kPasses];
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-        const int r = p * kRowsPerPass + r0;
-        const int64_t row = (int64_t)rt * kMxTileRows + r;
-        word[p] = row < rows ? *reinterpret_cast<const uint32_t *>(values + (uint64_t)row * L.pitch + c / 2) : 0u;
-        code[p] = row < rows ? scales[mx_scale_at((uint32_t)r, (uint32_t)lane16 >> 2)] : 0u;
+        for (int p = 0; p < kPasses; ++p) {
+            const bool in = p * kRowsPerPass < left;
+            word[p] = in ? reinterpret_cast<const uint32_t *>(from)[lane] : 0u;
+            code[p] = in ? scales[mx_scale_at((uint32_t)(p * kRowsPerPass + r0), (uint32_t)lane >> 2)] : 0u;
+            from += (uint64_t)kRowsPerPass * L.pitch;
+        }
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) {
+            if (p * kRowsPerPass >= left) break;
+            const float s = mx_scale_value(code[p]);
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = mx_element_value(mx_nibble(word[p], i)) * s;
+            store8(to, lane * 8, v);
+            to += (int64_t)kRowsPerPass * cols;
+        }
+        return;
     }
+    // rows that start anywhere: neighbouring lanes store neighbouring columns
+    for (int p = 0; p * kRowsPerPass < left; ++p) {
+        const uint32_t codes = *reinterpret_cast<const uint32_t *>(scales + mx_scale_at((uint32_t)(p * kRowsPerPass + r0), 0));
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-        const int64_t row = (int64_t)rt * kMxTileRows + p * kRowsPerPass + r0;
-        if (row >= rows) break;
-        const float s = mx_scale_value(code[p]);
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = mx_element_value(mx_nibble(word[p], i)) * s;
-        store8(out + row * cols, c, cols, whole, v);
+        for (int i = 0; i < 8; ++i) {
+            const int c = i * kLanes + lane;
+            if (c < width) {
+                const uint32_t word = reinterpret_cast<const uint32_t *>(from)[c >> 3];
+                const float v = mx_element_value(mx_nibble(word, c & 7)) * mx_scale_value(codes >> (8 * (c >> 5)) & 255u);
+                if constexpr (sizeof(T) == 2) to[c] = (uint16_t)tc::cvt_bf16x2(v, 0.f);
+                else to[c] = v;
+            }
+        }
+        from += (uint64_t)kRowsPerPass * L.pitch;
+        to += (int64_t)kRowsPerPass * cols;
     }
+}
+
+// The launch of either kernel.  Up to 64 columns: eight lanes a row instead of sixteen (the rest of the tile is not there).  Small matrices: a
+// tile in parts of 64, 32 or 16 rows, so that more SMs have work and a thread has fewer passes.
+struct Shape { int narrow, parts, whole; dim3 grid; };
+Shape shape_of(const npas_mx_desc &d, const MxLayout &L)
+{
+    Shape s;
+    s.narrow = d.cols <= 64;
+    s.whole = d.cols % 8 == 0;
+    s.parts = 1;
+    const uint64_t tiles = (uint64_t)L.nRT * L.nKT;
+    while (s.parts < (s.narrow ? 4 : 8) && tiles * s.parts * 2 <= 6ull * sm_count()) s.parts *= 2;
+    s.grid = dim3((unsigned)(tiles * s.parts));
+    return s;
+}
+template <typename T>
+cudaError_t quantize_any(const npas_mx_desc &d, const Shape &s, const void *src, void *blob, cudaStream_t st, Launch how)
+{
+    const auto kernel = s.narrow ? (s.parts > 1 ? quantize_mx_kernel<T, true, 8> : quantize_mx_kernel<T, false, 8>)
+                                 : (s.parts > 1 ? quantize_mx_kernel<T, true, 16> : quantize_mx_kernel<T, false, 16>);
+    return tc::launch_pdl(how, kernel, s.grid, dim3(kThreads), 0, st, (int)d.rows, (int)d.cols, s.whole, s.parts, static_cast<const T *>(src),
+                          static_cast<uint8_t *>(blob));
+}
+template <typename T>
+cudaError_t dequantize_any(const npas_mx_desc &d, const Shape &s, const void *blob, void *out, cudaStream_t st)
+{
+    const auto kernel = s.narrow ? (s.parts > 1 ? dequantize_mx_kernel<T, true, 8> : dequantize_mx_kernel<T, false, 8>)
+                                 : (s.parts > 1 ? dequantize_mx_kernel<T, true, 16> : dequantize_mx_kernel<T, false, 16>);
+    return tc::launch_pdl(Launch(), kernel, s.grid, dim3(kThreads), 0, st, (int)d.rows, (int)d.cols, s.whole, s.parts, static_cast<const uint8_t *>(blob),
+                          static_cast<T *>(out));
 }
 
 }  // namespace
 
 npas_status quantize_mx_launch(const npas_mx_desc &d, const void *src, void *blob, cudaStream_t st, Launch how)
 {
-    const MxLayout L = mx_layout(d.rows, d.cols);
-    const dim3 grid(L.nRT * L.nKT), block(kThreads);
-    const int whole = d.cols % 8 == 0;
-    cudaError_t e;
-    if (d.src_dtype == NPAS_BF16)
-        e = tc::launch_pdl(how, quantize_mx_kernel<uint16_t>, grid, block, 0, st, d.rows, d.cols, whole, static_cast<const uint16_t *>(src),
-                           static_cast<uint8_t *>(blob));
-    else
-        e = tc::launch_pdl(how, quantize_mx_kernel<float>, grid, block, 0, st, d.rows, d.cols, whole, static_cast<const float *>(src),
-                           static_cast<uint8_t *>(blob));
+    const Shape s = shape_of(d, mx_layout(d.rows, d.cols));
+    const cudaError_t e = d.src_dtype == NPAS_BF16 ? quantize_any<uint16_t>(d, s, src, blob, st, how) : quantize_any<float>(d, s, src, blob, st, how);
     count_launch();
     return e == cudaSuccess ? launch_status() : NPAS_ERR_CUDA;
 }
@@ -236,16 +320,9 @@ npas_status npas_dequantize_mx(const npas_mx_desc *d, const void *blob, size_t b
     const MxLayout L = mx_layout(d->rows, d->cols);
     if (blob_bytes < L.total) return NPAS_ERR_BUFFER_TOO_SMALL;
     if (blob == out) return NPAS_ERR_UNSUPPORTED;
-    const dim3 grid(L.nRT * L.nKT), block(kThreads);
-    const int whole = d->cols % 8 == 0;
+    const Shape f = shape_of(*d, L);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    cudaError_t e;
-    if (out_dtype == NPAS_BF16)
-        e = tc::launch_pdl(Launch(), dequantize_mx_kernel<uint16_t>, grid, block, 0, st, d->rows, d->cols, whole, static_cast<const uint8_t *>(blob),
-                           static_cast<uint16_t *>(out));
-    else
-        e = tc::launch_pdl(Launch(), dequantize_mx_kernel<float>, grid, block, 0, st, d->rows, d->cols, whole, static_cast<const uint8_t *>(blob),
-                           static_cast<float *>(out));
+    const cudaError_t e = out_dtype == NPAS_BF16 ? dequantize_any<uint16_t>(*d, f, blob, out, st) : dequantize_any<float>(*d, f, blob, out, st);
     count_launch();
     return e == cudaSuccess ? launch_status() : NPAS_ERR_CUDA;
 }
