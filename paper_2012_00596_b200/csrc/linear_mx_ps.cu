@@ -4,9 +4,14 @@
 // A CTA per SM walks tiles (outputs fastest, so that the rows of X of a tile are read from L2 by its neighbours).  Copies, MMAs, with a
 // 16-bit input the widening of the weights into tensor memory, and the epilogue are roles of their own that hand stages, slots and
 // accumulators on through barriers, so the next tile is loaded and multiplied while one is written out.  Two accumulators of 128 columns,
-// or one of 256 that the epilogue takes into registers before it does anything else (with 256 rows of X a weight is fetched half as
-// often, which long inputs need).  Tensor memory lane = output: a warp stores 32 consecutive outputs of a row of Y at a time, whatever
-// the alignment of Y's rows, and needs no shared memory for it; residuals are requested before the wait for the accumulator.
+// or one of 256 (with 256 rows of X a weight is fetched half as often, which long inputs need).
+//
+// Tensor memory lane = output, column = row of X, while a row of Y has its outputs side by side.  bf16 outputs whose rows start on 16-byte
+// boundaries go through shared memory: a warp takes 32 outputs x 32 rows out of tensor memory as 8 x 8 matrices, rounds pairs of rows
+// and stores them transposed (stmatrix) into a slab of 128 rows x 64 outputs, 128-byte swizzled, which leaves by TMA; residuals arrive
+// in the slab by TMA before and are read the same way, requested a ring of slots ahead.  2.3 instructions an output (4.3 with a
+// residual).  Other outputs (fp32, odd widths) are written from registers: 32 consecutive outputs of a row a warp, whatever the alignment,
+// residuals requested before the wait for the accumulator.
 // Every wait is bounded.
 #include <type_traits>
 
@@ -22,21 +27,24 @@ constexpr int kRows = 128;
 constexpr int kStepCols = 256;                             // columns of a weight stage
 constexpr int kMaxStages = 6, kMaxXStages = 8, kSlots = 4;
 constexpr uint32_t kSmemLimit = 232448;
+constexpr int kMaxSlots = 8;
 constexpr uint32_t kWBytes = kRows * 128;
+constexpr uint32_t kSlabBytes = kRows * 128;               // 128 rows x 64 outputs
 constexpr uint32_t kScaleBytes = 2 * kMxScaleTile;         // of 128 rows and a stage
 
-// warps: 0 copies, 1 MMAs, then a 16-bit input's own copies and the widening warps, then the epilogue
+// warps: 0 copies, 1 MMAs, then a 16-bit input's own copies and the widening warps, then the epilogue, one of them for the slabs' copies
 template <bool kMx> struct Roles {
     static constexpr int kXWarp = 2, kWideWarps = kMx ? 0 : 8, kFirstWide = 3;
-    static constexpr int kFirstEpi = kMx ? 2 : kFirstWide + kWideWarps + 1;          // (a multiple of four behind the 16-bit roles)
-    static constexpr int kEpiWarps = kMx ? 16 : 8;
-    static constexpr int kThreads = (kFirstEpi + kEpiWarps) * 32;
+    static constexpr int kFirstEpi = kMx ? 2 : kFirstWide + kWideWarps + 1;
+    static constexpr int kEpiWarps = kMx ? 16 : 8, kParts = kEpiWarps / 4;
+    static constexpr int kStoreWarp = kMx ? kFirstEpi + kEpiWarps : kFirstWide + kWideWarps;
+    static constexpr int kThreads = (kFirstEpi + kEpiWarps + (kMx ? 1 : 0)) * 32;
 };
 
 struct MxPsParams {
-    int M, I, O, N, acc, nS, nMT, nOT, n_tiles, nKT, S, SX;    // acc: accumulators; SX: stages of the input (16 bits)
+    int M, I, O, N, acc, nS, nMT, nOT, n_tiles, nKT, S, SX, NS;  // acc: accumulators; SX: stages of the input (16 bits); NS: slabs (a power of two; 0: none)
     int relu, y_bf16;
-    uint32_t x_bytes, xs_bytes, stage_bytes, off_x, off_bar, smem_bytes, tmem_cols, tmem_scales, scale_cols;
+    uint32_t x_bytes, xs_bytes, stage_bytes, off_x, off_slabs, off_bar, smem_bytes, tmem_cols, tmem_scales, scale_cols;
     uint64_t w_scales, x_scales;                           // offsets of the scales in the blobs
 };
 
@@ -45,28 +53,10 @@ struct MxPsBars {
     uint64_t x_full[kMaxXStages], x_empty[kMaxXStages];
     uint64_t slot_full[kSlots], slot_empty[kSlots];
     uint64_t acc_full[2], acc_empty[2];
+    uint64_t slab_ready[kMaxSlots], slab_done[kMaxSlots];  // free (or its residuals have landed) / every epilogue warp has finished its part
     uint32_t tmem_base;
     uint32_t abort_flag;
 };
-
-// 64 columns of a row: two 16-byte pieces of elements, two scale codes -> 32 pairs of bf16 values
-__device__ __forceinline__ void widen(uint32_t (&r)[32], const uint4 &a, const uint4 &b, uint32_t code0, uint32_t code1)
-{
-    const MxFactor f0 = mx_factor(code0), f1 = mx_factor(code1);
-    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t f = j < 4 ? f0.first : f1.first;
-        r[4 * j] = mul_bf16x2(mx_pair_small<0>(w[j]), f);
-        r[4 * j + 1] = mul_bf16x2(mx_pair_small<1>(w[j]), f);
-        r[4 * j + 2] = mul_bf16x2(mx_pair_small<2>(w[j]), f);
-        r[4 * j + 3] = mul_bf16x2(mx_pair_small<3>(w[j]), f);
-    }
-    if (__any_sync(0xFFFFFFFFu, code0 > 128u || code1 > 128u)) {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) r[j] = mul_bf16x2(r[j], j < 16 ? f0.second : f1.second);
-    }
-}
 
 // 32 rows of one output: bias + residuals, then sums + those, ReLU, one rounding.  `at`: element of the first row; `n`: rows there are
 // (none where the output lies past the end).
@@ -109,7 +99,8 @@ __device__ __forceinline__ void store_rows(const uint32_t (&v)[32], float b, voi
 
 template <bool kMx, bool kBf16>
 __global__ void __launch_bounds__(Roles<kMx>::kThreads, 1)
-linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w, const MxPsParams p, const uint8_t *xblob,
+linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_y,
+                    const __grid_constant__ CUtensorMap tmap_r, const MxPsParams p, const uint8_t *xblob,
                     const uint8_t *wblob, const float *bias, const void *res, void *y, uint32_t *ws)
 {
     using R = Roles<kMx>;
@@ -125,10 +116,12 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
         for (int s = 0; s < p.SX; ++s) { mbar_init(&bars->x_full[s], 1); mbar_init(&bars->x_empty[s], 1); }
         for (int s = 0; s < kSlots; ++s) { mbar_init(&bars->slot_full[s], 4); mbar_init(&bars->slot_empty[s], 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(&bars->acc_full[a], 1); mbar_init(&bars->acc_empty[a], R::kEpiWarps); }
+        for (int n = 0; n < p.NS; ++n) { mbar_init(&bars->slab_ready[n], 1); mbar_init(&bars->slab_done[n], R::kEpiWarps / 2); }
         bars->abort_flag = 0;
         fence_barrier_init();
         prefetch_tensormap(&tmap_x);
         prefetch_tensormap(&tmap_w);
+        if (p.NS) { prefetch_tensormap(&tmap_y); if (res) prefetch_tensormap(&tmap_r); }
     }
     if (warp == 1) tmem_alloc(&bars->tmem_base, p.tmem_cols);
     pdl_trigger();
@@ -244,7 +237,7 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
                     const uint4 b = *reinterpret_cast<const uint4 *>(st + r * 128 + ((2 * q + 1) ^ (r & 7)) * 16);
                     const uint32_t codes = *reinterpret_cast<const uint32_t *>(st + kWBytes + (q >> 1) * kMxScaleTile + lane * 16 + quarter * 4) >> (16 * (q & 1));
                     uint32_t v[32];
-                    widen(v, a, b, codes & 255u, (codes >> 8) & 255u);
+                    mx_widen(v, a, b, codes & 255u, (codes >> 8) & 255u);
                     if (k >= kSlots) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->slot_empty[slot], ((k / kSlots) & 1u) ^ 1u, abort_flag, ws, 0xB410));
                     if (!ok) break;
                     tc_fence_after_sync();
@@ -260,8 +253,117 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
                 if (++s == (uint32_t)p.S) { s = 0; ph ^= 1u; }
             }
         }
+    } else if (warp == R::kStoreWarp) {
+        // ---- slabs: one leaves by TMA as soon as every epilogue warp has finished its part; when the store before it has been read,
+        // that slab is free again, or takes the residuals of the slab a ring further on ----------------------------------------
+        if (lane == 0 && p.NS) {
+            // the slabs of this CTA's tiles in order: (tile, 128 rows, 64 outputs), those that exist
+            struct Walk {
+                int tile, r, h;
+                __device__ bool begin(const MxPsParams &p, int t) { tile = t; r = h = 0; return tile < p.n_tiles; }
+                __device__ int row(const MxPsParams &p) const { return tile / p.nOT * p.N + r * kRows; }
+                __device__ int col(const MxPsParams &p) const { return tile % p.nOT * kRows + h * 64; }
+                __device__ bool next(const MxPsParams &p)
+                {
+                    if (h == 0) { h = 1; if (col(p) < p.O) return true; }
+                    h = 0; ++r;
+                    if (r * kRows < p.N && row(p) < p.M) return true;
+                    r = 0; tile += gridDim.x;
+                    return tile < p.n_tiles;
+                }
+            };
+            auto request = [&](const Walk &w, uint32_t n) {
+                uint64_t *bar = &bars->slab_ready[n & (p.NS - 1)];
+                mbar_arrive_expect_tx(bar, kSlabBytes);
+                tma_load_2d(smem + p.off_slabs + (size_t)(n & (p.NS - 1)) * kSlabBytes, &tmap_r, bar, w.col(p), w.row(p));
+            };
+            Walk w, ahead;
+            bool more = w.begin(p, blockIdx.x), more_ahead = ahead.begin(p, blockIdx.x);
+            uint32_t n = 0, asked = 0;
+            for (; res && asked < (uint32_t)p.NS && more_ahead; ++asked) { request(ahead, asked); more_ahead = ahead.next(p); }
+            for (; more; ++n) {
+                if (!mbar_wait(&bars->slab_done[n & (p.NS - 1)], (n / p.NS) & 1u, abort_flag, ws, 0xB600)) break;
+                tma_store_2d(&tmap_y, smem + p.off_slabs + (size_t)(n & (p.NS - 1)) * kSlabBytes, w.col(p), w.row(p));
+                bulk_commit();
+                if (n) {
+                    bulk_wait_read<1>();
+                    if (!res) mbar_arrive(&bars->slab_ready[(n - 1) & (p.NS - 1)]);
+                    else if (more_ahead) { request(ahead, asked++); more_ahead = ahead.next(p); }     // (slab n - 1 + NS)
+                }
+                more = w.next(p);
+            }
+            bulk_wait_read<0>();                               // the slabs stay valid until the last store has read them
+        }
+    } else if (warp >= R::kFirstEpi && p.NS) {
+        // ---- epilogue through slabs: warp -> lane quarter, and a share of every 128 columns ---------------------------------
+        const int quarter = warp & 3, part = (warp - R::kFirstEpi) >> 2, half = quarter >> 1;
+        constexpr int kShare = kRows / R::kParts;
+        // this lane's row and 16-byte piece in the slab: row (lane % 8) of 8 x 8 matrix (lane / 8)
+        const uint32_t lane_at = smem_u32(smem) + p.off_slabs + (uint32_t)((part * kShare + (lane & 7)) * 128 + ((((quarter & 1) * 4 + (lane >> 3)) ^ (lane & 7)) * 16));
+        uint32_t it = 0, n = 0;                                // n: slabs of the tiles before
+        bool ok = true;
+        for (int tile = blockIdx.x; tile < p.n_tiles && ok; tile += gridDim.x, ++it) {
+            const int mt = tile / p.nOT, ot = tile - mt * p.nOT, o0 = ot * kRows + quarter * 32 + (lane >> 2);
+            const uint32_t acc = p.acc == 2 ? it & 1u : 0u, lap = p.acc == 2 ? it >> 1 : it;
+            const int halves = ot * kRows + 64 < p.O ? 2 : 1, blocks = min(p.N, p.M - mt * p.N + kRows - 1) / kRows;
+            float b[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) b[i] = bias && o0 + 8 * i < p.O ? __ldg(bias + o0 + 8 * i + z) : 0.f;
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->acc_full[acc], lap & 1u, abort_flag, ws, 0xB500));
+            if (!ok) break;
+            tc_fence_after_sync();
+            const uint32_t t_addr = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * p.N + (uint32_t)(part * kShare);
+            for (int r = 0; r < blocks && half < halves && ok; ++r) {
+                const uint32_t at = n + (uint32_t)(r * halves + half), slot = at & (p.NS - 1), slab = lane_at + slot * kSlabBytes;
+                const uint32_t use = at / p.NS;
+                // with residuals: they have landed; without: the store that last used the slab has read it (from its second use on)
+                if (res || use) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->slab_ready[slot], (res ? use : use - 1) & 1u, abort_flag, ws, 0xB510));
+                if (!ok) break;
+#pragma unroll
+                for (int c = 0; c < kShare; c += 32) {
+                    uint32_t u[16], v[16];                     // outputs 0 to 15 and 16 to 31 of the quarter
+                    tmem_ld_16x32(t_addr + r * kRows + c, u);
+                    tmem_ld_16x32(t_addr + r * kRows + c + (16u << 16), v);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {              // eight rows of Y
+                        float f[8] = {__uint_as_float(u[4 * k]) + b[0], __uint_as_float(u[4 * k + 1]) + b[0], __uint_as_float(u[4 * k + 2]) + b[1],
+                                      __uint_as_float(u[4 * k + 3]) + b[1], __uint_as_float(v[4 * k]) + b[2], __uint_as_float(v[4 * k + 1]) + b[2],
+                                      __uint_as_float(v[4 * k + 2]) + b[3], __uint_as_float(v[4 * k + 3]) + b[3]};
+                        const uint32_t sa = slab + (uint32_t)(c + 8 * k) * 128u;
+                        if (res) {
+                            uint32_t q[4];
+                            ldmatrix_x4_trans(sa, q);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                f[2 * i] += __uint_as_float(q[i] << 16);
+                                f[2 * i + 1] += __uint_as_float(q[i] & 0xFFFF0000u);
+                            }
+                        }
+                        // one rounding, then ReLU on the rounded pairs (max with +0 is exact on them)
+                        uint32_t w[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            w[i] = cvt_bf16x2(f[2 * i], f[2 * i + 1]);
+                            if (p.relu) w[i] = relu_bf16x2(w[i]);
+                        }
+                        if (res) __syncwarp();                 // (every lane has read these rows' residuals)
+                        stmatrix_x4_trans(sa, w[0], w[1], w[2], w[3]);
+                    }
+                }
+                fence_proxy_async_smem();                      // the TMA store reads what this thread wrote
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars->slab_done[slot]);
+            }
+            n += (uint32_t)(halves * blocks);
+            if (!ok) break;
+            // this warp has read its part of the accumulator: the MMA warp may overwrite it
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars->acc_empty[acc]);
+        }
     } else if (warp >= R::kFirstEpi) {
-        // ---- epilogue: warp -> lane quarter and a share of the accumulator's columns -------------------------------------
+        // ---- epilogue from registers: warp -> lane quarter and a share of the accumulator's columns -------------------------------------
         const int quarter = warp & 3, part = (warp - R::kFirstEpi) >> 2, share = p.N / (R::kEpiWarps / 4);
         uint32_t it = 0;
         for (int tile = blockIdx.x; tile < p.n_tiles; tile += gridDim.x, ++it) {
@@ -345,12 +447,16 @@ bool plan(const npas_mx_linear_desc &d, MxPsParams &p, int sms)
     p.xs_bytes = mx ? (uint32_t)p.N / kRows * kScaleBytes : 0u;
     p.stage_bytes = round_up(kWBytes + kScaleBytes + (mx ? p.xs_bytes + p.x_bytes : 0u), 1024);
     const uint32_t budget = kSmemLimit - (uint32_t)sizeof(MxPsBars) - 128u - 1024u;
-    if (!mx) p.SX = p.N == 256 ? 4 : 8;
-    p.S = (int)((budget - (uint32_t)p.SX * p.x_bytes) / p.stage_bytes);
+    // Slabs for bf16 outputs with rows on 16-byte boundaries: four, eight where residuals are ahead of little else; and the input's ring
+    p.NS = p.y_bf16 && d.O % 8 == 0 ? (mx && d.has_residual && p.nS <= 2 && p.N == 128 ? 8 : 4) : 0;
+    if (!mx) p.SX = p.N == 256 ? 3 : 6;
+    const uint32_t fixed = (uint32_t)p.SX * p.x_bytes + (uint32_t)p.NS * kSlabBytes;
+    p.S = (int)((budget - fixed) / p.stage_bytes);
     if (p.S > kMaxStages) p.S = kMaxStages;
     if (p.S < 2) return false;
     p.off_x = (uint32_t)p.S * p.stage_bytes;
-    p.off_bar = round_up(p.off_x + (uint32_t)p.SX * p.x_bytes, 128);
+    p.off_slabs = p.off_x + (uint32_t)p.SX * p.x_bytes;
+    p.off_bar = round_up(p.off_slabs + (uint32_t)p.NS * kSlabBytes, 128);
     p.smem_bytes = p.off_bar + (uint32_t)sizeof(MxPsBars) + 1024u;
     if (p.smem_bytes > kSmemLimit) return false;
     p.tmem_scales = 256;
@@ -386,12 +492,16 @@ npas_status linear_mx_ps_launch(const npas_mx_linear_desc &d, const void *x, int
     if (!(mx ? mx_encode_values(&tmx, x, mx_layout(d.M, d.I), d.M, (uint32_t)p.N)
              : mx_encode_bf16(&tmx, x, (uint64_t)d.I, (uint64_t)x_pitch, (uint64_t)d.M, (uint32_t)p.N)))
         return NPAS_ERR_CUDA;
+    CUtensorMap tmy = tmx, tmr = tmx;
+    if (p.NS && (!mx_encode_bf16(&tmy, y, (uint64_t)d.O, (uint64_t)d.O, (uint64_t)d.M, kRows) ||
+                 (res && !mx_encode_bf16(&tmr, res, (uint64_t)d.O, (uint64_t)d.O, (uint64_t)d.M, kRows))))
+        return NPAS_ERR_CUDA;
     const auto kernel = mx ? (p.y_bf16 ? linear_mx_ps_kernel<true, true> : linear_mx_ps_kernel<true, false>)
                            : (p.y_bf16 ? linear_mx_ps_kernel<false, true> : linear_mx_ps_kernel<false, false>);
     if (allow_dynamic_smem(reinterpret_cast<const void *>(kernel), (int)kSmemLimit) != NPAS_OK) return NPAS_ERR_CUDA;
     const int sms = sm_count();
     const cudaError_t e = launch_pdl(Launch(), kernel, dim3((unsigned)(p.n_tiles < sms ? p.n_tiles : sms)), dim3(mx ? Roles<true>::kThreads : Roles<false>::kThreads),
-                                     p.smem_bytes, st, tmx, tmw, p, static_cast<const uint8_t *>(x), static_cast<const uint8_t *>(w), bias, res, y, ws);
+                                     p.smem_bytes, st, tmx, tmw, tmy, tmr, p, static_cast<const uint8_t *>(x), static_cast<const uint8_t *>(w), bias, res, y, ws);
     count_launch();
     return e == cudaSuccess ? launch_status() : NPAS_ERR_CUDA;
 }

@@ -61,25 +61,6 @@ __device__ __forceinline__ void store_y(void *y, int64_t at, float v, int relu, 
     else static_cast<float *>(y)[at] = v;
 }
 
-// 64 columns of a row: two 16-byte pieces of elements, two scale codes -> 32 pairs of bf16 values
-__device__ __forceinline__ void widen(uint32_t (&r)[32], const uint4 &a, const uint4 &b, uint32_t code0, uint32_t code1)
-{
-    const MxFactor f0 = mx_factor(code0), f1 = mx_factor(code1);
-    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t f = j < 4 ? f0.first : f1.first;
-        r[4 * j] = mul_bf16x2(mx_pair_small<0>(w[j]), f);
-        r[4 * j + 1] = mul_bf16x2(mx_pair_small<1>(w[j]), f);
-        r[4 * j + 2] = mul_bf16x2(mx_pair_small<2>(w[j]), f);
-        r[4 * j + 3] = mul_bf16x2(mx_pair_small<3>(w[j]), f);
-    }
-    if (__any_sync(0xFFFFFFFFu, code0 > 128u || code1 > 128u)) {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) r[j] = mul_bf16x2(r[j], j < 16 ? f0.second : f1.second);
-    }
-}
-
 template <bool kMx>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w, const MxSwParams p, const uint8_t *xblob,
@@ -210,7 +191,7 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
                 const uint4 b = *reinterpret_cast<const uint4 *>(st + r * 128 + ((2 * q + 1) ^ (r & 7)) * 16);
                 const uint32_t codes = *reinterpret_cast<const uint32_t *>(st + kWBytes + (q >> 1) * kMxScaleTile + lane * 16 + quarter * 4) >> (16 * (q & 1));
                 uint32_t v[32];
-                widen(v, a, b, codes & 255u, (codes >> 8) & 255u);
+                mx_widen(v, a, b, codes & 255u, (codes >> 8) & 255u);
                 if (k >= kSlots) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->slot_empty[slot], ((k / kSlots) & 1u) ^ 1u, abort_flag, ws, 0xA410));
                 if (!ok) break;
                 tc_fence_after_sync();

@@ -61,6 +61,34 @@ __device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t (&r)[
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// 16 lanes x 32 consecutive 32-bit columns: thread t gets, for k = 0..3, columns 8k + 2 (t % 4) and the next of lane t / 4 (r[4k], r[4k + 1])
+// and of lane t / 4 + 8 (r[4k + 2], r[4k + 3]): the layout of 8 x 8 matrices that stmatrix takes.
+__device__ __forceinline__ void tmem_ld_16x32(uint32_t taddr, uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
+}
+// four 8 x 8 matrices of 16-bit values, transposed: lane l gives the address of row l % 8 of matrix l / 8
+__device__ __forceinline__ void stmatrix_x4_trans(uint32_t saddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(saddr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t saddr, uint32_t (&r)[4])
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(saddr) : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *m, const void *src, int c0, int c1)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];"
+                 ::"l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(src)), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
 {
     uint32_t d;
@@ -88,6 +116,25 @@ __device__ __forceinline__ MxFactor mx_factor(uint32_t code)
     return f;
 }
 
+// 64 columns of a row: two 16-byte pieces of elements, two scale codes -> 32 pairs of bf16 values
+__device__ __forceinline__ void mx_widen(uint32_t (&r)[32], const uint4 &a, const uint4 &b, uint32_t code0, uint32_t code1)
+{
+    const MxFactor f0 = mx_factor(code0), f1 = mx_factor(code1);
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t f = j < 4 ? f0.first : f1.first;
+        r[4 * j] = mul_bf16x2(mx_pair_small<0>(w[j]), f);
+        r[4 * j + 1] = mul_bf16x2(mx_pair_small<1>(w[j]), f);
+        r[4 * j + 2] = mul_bf16x2(mx_pair_small<2>(w[j]), f);
+        r[4 * j + 3] = mul_bf16x2(mx_pair_small<3>(w[j]), f);
+    }
+    if (__any_sync(0xFFFFFFFFu, code0 > 128u || code1 > 128u)) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) r[j] = mul_bf16x2(r[j], j < 16 ? f0.second : f1.second);
+    }
+}
+
 // ---- host: tensor maps ------------------------------------------------------------------------
 // values of a blob: bytes, boxes of 128 bytes (256 columns) x rows, 128-byte swizzled, past the end zeros
 inline bool mx_encode_values(CUtensorMap *map, const void *blob, const MxLayout &L, int rows, uint32_t box_rows)
@@ -99,7 +146,7 @@ inline bool mx_encode_values(CUtensorMap *map, const void *blob, const MxLayout 
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(static_cast<const uint8_t *>(blob)) + L.off_values, dims, strides, box, estr,
                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// a bf16 matrix with rows of `pitch` elements (a multiple of 8): boxes of 64 columns x rows, 128-byte swizzled, past the end zeros
+// a bf16 matrix with rows of `pitch` elements (a multiple of 8; inputs, outputs, residuals): boxes of 64 columns x rows, 128-byte swizzled, past the end zeros
 inline bool mx_encode_bf16(CUtensorMap *map, const void *base, uint64_t cols, uint64_t pitch, uint64_t rows, uint32_t box_rows)
 {
     EncodeTiledFn enc = encode_tiled_fn();
