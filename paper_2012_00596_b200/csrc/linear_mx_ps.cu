@@ -36,13 +36,15 @@ constexpr uint32_t kScaleBytes = 2 * kMxScaleTile;         // of 128 rows and a 
 template <bool kMx> struct Roles {
     static constexpr int kXWarp = 2, kWideWarps = kMx ? 0 : 8, kFirstWide = 3;
     static constexpr int kFirstEpi = kMx ? 2 : kFirstWide + kWideWarps + 1;
-    static constexpr int kEpiWarps = kMx ? 16 : 8, kParts = kEpiWarps / 4;
+    static constexpr int kEpiWarps = kMx ? 16 : 8, kGroups = kEpiWarps / 8;
     static constexpr int kStoreWarp = kMx ? kFirstEpi + kEpiWarps : kFirstWide + kWideWarps;
     static constexpr int kThreads = (kFirstEpi + kEpiWarps + (kMx ? 1 : 0)) * 32;
 };
 
 struct MxPsParams {
-    int M, I, O, N, acc, nS, nMT, nOT, n_tiles, nKT, S, SX, NS;  // acc: accumulators; SX: stages of the input (16 bits); NS: slabs (a power of two; 0: none)
+    int M, I, O, N, acc, nS, nMT, nOT, n_tiles, nKT, S, SX, NS, ns_log;
+    // acc: accumulators; SX: stages of the input (16 bits); NS = 2^ns_log: slabs (0: none)
+    int grid, step_mt, step_ot;                                  // a CTA's way from tile to tile
     int relu, y_bf16;
     uint32_t x_bytes, xs_bytes, stage_bytes, off_x, off_slabs, off_bar, smem_bytes, tmem_cols, tmem_scales, scale_cols;
     uint64_t w_scales, x_scales;                           // offsets of the scales in the blobs
@@ -80,13 +82,13 @@ __device__ __forceinline__ void load_residuals(float (&add)[32], float b, const 
     for (int i = 0; i < 32; ++i) add[i] += b;
 }
 template <bool kBf16>
-__device__ __forceinline__ void store_rows(const uint32_t (&v)[32], float b, void *y, int64_t at, int64_t O, int n, int relu)
+__device__ __forceinline__ void store_rows(const uint32_t (&v)[32], const float (&add)[32], void *y, int64_t at, int64_t O, int n, int relu)
 {
     using T = typename std::conditional<kBf16, uint16_t, float>::type;
     T *q = static_cast<T *>(y) + at;
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
-        float u = __uint_as_float(v[i]) + b;
+        float u = __uint_as_float(v[i]) + add[i];
         if (relu) u = fmaxf(u, 0.f);
         if (i < n) {
             if constexpr (kBf16) *q = (uint16_t)cvt_bf16x2(u, 0.f);
@@ -96,6 +98,21 @@ __device__ __forceinline__ void store_rows(const uint32_t (&v)[32], float b, voi
         asm volatile("" : "+l"(q));
     }
 }
+
+// the tiles of a CTA (the coordinates are carried along: two divisions a tile take longer than some roles' work on it)
+struct TileWalk {
+    int tile, mt, ot;
+    __device__ __forceinline__ explicit TileWalk(const MxPsParams &p) : tile(blockIdx.x), mt(blockIdx.x / p.nOT), ot(blockIdx.x - mt * p.nOT) {}
+    __device__ __forceinline__ bool in(const MxPsParams &p) const { return tile < p.n_tiles; }
+    __device__ __forceinline__ void next(const MxPsParams &p)
+    {
+        tile += gridDim.x; mt += p.step_mt; ot += p.step_ot;
+        if (ot >= p.nOT) { ot -= p.nOT; ++mt; }
+    }
+    // blocks of 128 rows and halves of 64 outputs that exist
+    __device__ __forceinline__ int blocks(const MxPsParams &p) const { return min(p.N / kRows, (p.M - mt * p.N + kRows - 1) / kRows); }
+    __device__ __forceinline__ int halves(const MxPsParams &p) const { return ot * kRows + 64 < p.O ? 2 : 1; }
+};
 
 template <bool kMx, bool kBf16>
 __global__ void __launch_bounds__(Roles<kMx>::kThreads, 1)
@@ -115,8 +132,8 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
         for (int s = 0; s < p.S; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], kMx ? 1 : R::kWideWarps); }
         for (int s = 0; s < p.SX; ++s) { mbar_init(&bars->x_full[s], 1); mbar_init(&bars->x_empty[s], 1); }
         for (int s = 0; s < kSlots; ++s) { mbar_init(&bars->slot_full[s], 4); mbar_init(&bars->slot_empty[s], 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(&bars->acc_full[a], 1); mbar_init(&bars->acc_empty[a], R::kEpiWarps); }
-        for (int n = 0; n < p.NS; ++n) { mbar_init(&bars->slab_ready[n], 1); mbar_init(&bars->slab_done[n], R::kEpiWarps / 2); }
+        for (int a = 0; a < 2; ++a) { mbar_init(&bars->acc_full[a], 1); mbar_init(&bars->acc_empty[a], p.acc == 2 ? 8 : R::kEpiWarps); }
+        for (int n = 0; n < p.NS; ++n) { mbar_init(&bars->slab_ready[n], 1); mbar_init(&bars->slab_done[n], 4); }
         bars->abort_flag = 0;
         fence_barrier_init();
         prefetch_tensormap(&tmap_x);
@@ -136,8 +153,8 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
         if (lane == 0) {
             uint32_t s = 0, lap = 0;
             bool ok = true;
-            for (int tile = blockIdx.x; tile < p.n_tiles && ok; tile += gridDim.x) {
-                const int mt = tile / p.nOT, ot = tile - mt * p.nOT;
+            for (TileWalk w(p); w.in(p) && ok; w.next(p)) {
+                const int mt = w.mt, ot = w.ot;
                 for (int step = 0; step < p.nS; ++step) {
                     if (lap >= 1 && !mbar_wait(&bars->empty[s], (lap & 1u) ^ 1u, abort_flag, ws, 0xB100)) { ok = false; break; }
                     uint8_t *st = smem + (size_t)s * p.stage_bytes;
@@ -210,12 +227,11 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
         if (lane == 0) {
             uint32_t s = 0, lap = 0;
             bool ok = true;
-            for (int tile = blockIdx.x; tile < p.n_tiles && ok; tile += gridDim.x) {
-                const int mt = tile / p.nOT;
+            for (TileWalk w(p); w.in(p) && ok; w.next(p)) {
                 for (int k = 0; k < nK; ++k) {
                     if (lap >= 1 && !mbar_wait(&bars->x_empty[s], (lap & 1u) ^ 1u, abort_flag, ws, 0xB110)) { ok = false; break; }
                     mbar_arrive_expect_tx(&bars->x_full[s], p.x_bytes);
-                    tma_load_2d(smem + p.off_x + (size_t)s * p.x_bytes, &tmap_x, &bars->x_full[s], k * 64, mt * p.N);
+                    tma_load_2d(smem + p.off_x + (size_t)s * p.x_bytes, &tmap_x, &bars->x_full[s], k * 64, w.mt * p.N);
                     if (++s == (uint32_t)p.SX) { s = 0; ++lap; }
                 }
             }
@@ -259,68 +275,73 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
         if (lane == 0 && p.NS) {
             // the slabs of this CTA's tiles in order: (tile, 128 rows, 64 outputs), those that exist
             struct Walk {
-                int tile, r, h;
-                __device__ bool begin(const MxPsParams &p, int t) { tile = t; r = h = 0; return tile < p.n_tiles; }
-                __device__ int row(const MxPsParams &p) const { return tile / p.nOT * p.N + r * kRows; }
-                __device__ int col(const MxPsParams &p) const { return tile % p.nOT * kRows + h * 64; }
-                __device__ bool next(const MxPsParams &p)
+                TileWalk t;
+                int r, h, blocks, halves;
+                bool more;
+                __device__ explicit Walk(const MxPsParams &p) : t(p), r(0), h(0), blocks(t.blocks(p)), halves(t.halves(p)), more(t.in(p)) {}
+                __device__ void next(const MxPsParams &p)
                 {
-                    if (h == 0) { h = 1; if (col(p) < p.O) return true; }
-                    h = 0; ++r;
-                    if (r * kRows < p.N && row(p) < p.M) return true;
-                    r = 0; tile += gridDim.x;
-                    return tile < p.n_tiles;
+                    if (++h < halves) return;
+                    h = 0;
+                    if (++r < blocks) return;
+                    r = 0;
+                    t.next(p);
+                    more = t.in(p); blocks = t.blocks(p); halves = t.halves(p);
                 }
+                __device__ int row(const MxPsParams &p) const { return t.mt * p.N + r * kRows; }
+                __device__ int col(const MxPsParams &) const { return t.ot * kRows + h * 64; }
             };
+            const uint32_t mask = (uint32_t)p.NS - 1;
             auto request = [&](const Walk &w, uint32_t n) {
-                uint64_t *bar = &bars->slab_ready[n & (p.NS - 1)];
+                uint64_t *bar = &bars->slab_ready[n & mask];
                 mbar_arrive_expect_tx(bar, kSlabBytes);
-                tma_load_2d(smem + p.off_slabs + (size_t)(n & (p.NS - 1)) * kSlabBytes, &tmap_r, bar, w.col(p), w.row(p));
+                tma_load_2d(smem + p.off_slabs + (size_t)(n & mask) * kSlabBytes, &tmap_r, bar, w.col(p), w.row(p));
             };
-            Walk w, ahead;
-            bool more = w.begin(p, blockIdx.x), more_ahead = ahead.begin(p, blockIdx.x);
+            Walk ahead(p);
             uint32_t n = 0, asked = 0;
-            for (; res && asked < (uint32_t)p.NS && more_ahead; ++asked) { request(ahead, asked); more_ahead = ahead.next(p); }
-            for (; more; ++n) {
-                if (!mbar_wait(&bars->slab_done[n & (p.NS - 1)], (n / p.NS) & 1u, abort_flag, ws, 0xB600)) break;
-                tma_store_2d(&tmap_y, smem + p.off_slabs + (size_t)(n & (p.NS - 1)) * kSlabBytes, w.col(p), w.row(p));
+            for (; res && asked < (uint32_t)p.NS && ahead.more; ++asked) { request(ahead, asked); ahead.next(p); }
+            for (Walk w(p); w.more; w.next(p), ++n) {
+                if (!mbar_wait(&bars->slab_done[n & mask], (n >> p.ns_log) & 1u, abort_flag, ws, 0xB600)) break;
+                tma_store_2d(&tmap_y, smem + p.off_slabs + (size_t)(n & mask) * kSlabBytes, w.col(p), w.row(p));
                 bulk_commit();
                 if (n) {
                     bulk_wait_read<1>();
-                    if (!res) mbar_arrive(&bars->slab_ready[(n - 1) & (p.NS - 1)]);
-                    else if (more_ahead) { request(ahead, asked++); more_ahead = ahead.next(p); }     // (slab n - 1 + NS)
+                    if (!res) mbar_arrive(&bars->slab_ready[(n - 1) & mask]);
+                    else if (ahead.more) { request(ahead, asked++); ahead.next(p); }     // (slab n - 1 + NS)
                 }
-                more = w.next(p);
             }
             bulk_wait_read<0>();                               // the slabs stay valid until the last store has read them
         }
     } else if (warp >= R::kFirstEpi && p.NS) {
-        // ---- epilogue through slabs: warp -> lane quarter, and a share of every 128 columns ---------------------------------
-        const int quarter = warp & 3, part = (warp - R::kFirstEpi) >> 2, half = quarter >> 1;
-        constexpr int kShare = kRows / R::kParts;
+        // ---- epilogue through slabs.  Groups of eight warps: with two accumulators a group has every other tile (while one waits for
+        // tensor memory or a barrier the other one computes), with one accumulator a block of 128 rows of every tile.  Warp -> lane
+        // quarter and 64 of a block's 128 rows -----------------------------------------------------------------------------
+        const int e = warp - R::kFirstEpi, group = e >> 3, quarter = warp & 3, part = (e >> 2) & 1, half = quarter >> 1;
         // this lane's row and 16-byte piece in the slab: row (lane % 8) of 8 x 8 matrix (lane / 8)
-        const uint32_t lane_at = smem_u32(smem) + p.off_slabs + (uint32_t)((part * kShare + (lane & 7)) * 128 + ((((quarter & 1) * 4 + (lane >> 3)) ^ (lane & 7)) * 16));
+        const uint32_t lane_at = smem_u32(smem) + p.off_slabs + (uint32_t)((part * 64 + (lane & 7)) * 128 + ((((quarter & 1) * 4 + (lane >> 3)) ^ (lane & 7)) * 16));
         uint32_t it = 0, n = 0;                                // n: slabs of the tiles before
         bool ok = true;
-        for (int tile = blockIdx.x; tile < p.n_tiles && ok; tile += gridDim.x, ++it) {
-            const int mt = tile / p.nOT, ot = tile - mt * p.nOT, o0 = ot * kRows + quarter * 32 + (lane >> 2);
+        for (TileWalk w(p); w.in(p) && ok; w.next(p), ++it) {
+            const int halves = w.halves(p), blocks = w.blocks(p);
+            const uint32_t n_tile = n;
+            n += (uint32_t)(halves * blocks);
+            if (p.acc == 2 && R::kGroups == 2 && (it & 1u) != (uint32_t)group) continue;
+            const int o0 = w.ot * kRows + quarter * 32 + (lane >> 2);
             const uint32_t acc = p.acc == 2 ? it & 1u : 0u, lap = p.acc == 2 ? it >> 1 : it;
-            const int halves = ot * kRows + 64 < p.O ? 2 : 1, blocks = min(p.N, p.M - mt * p.N + kRows - 1) / kRows;
             float b[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) b[i] = bias && o0 + 8 * i < p.O ? __ldg(bias + o0 + 8 * i + z) : 0.f;
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->acc_full[acc], lap & 1u, abort_flag, ws, 0xB500));
             if (!ok) break;
             tc_fence_after_sync();
-            const uint32_t t_addr = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * p.N + (uint32_t)(part * kShare);
-            for (int r = 0; r < blocks && half < halves && ok; ++r) {
-                const uint32_t at = n + (uint32_t)(r * halves + half), slot = at & (p.NS - 1), slab = lane_at + slot * kSlabBytes;
-                const uint32_t use = at / p.NS;
+            const uint32_t t_addr = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * p.N + (uint32_t)(part * 64);
+            for (int r = p.acc == 1 && R::kGroups == 2 ? group : 0; r < blocks && half < halves && ok; r += p.acc == 1 ? R::kGroups : 1) {
+                const uint32_t at = n_tile + (uint32_t)(r * halves + half), slot = at & (p.NS - 1), slab = lane_at + slot * kSlabBytes, use = at >> p.ns_log;
                 // with residuals: they have landed; without: the store that last used the slab has read it (from its second use on)
                 if (res || use) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->slab_ready[slot], (res ? use : use - 1) & 1u, abort_flag, ws, 0xB510));
                 if (!ok) break;
 #pragma unroll
-                for (int c = 0; c < kShare; c += 32) {
+                for (int c = 0; c < 64; c += 32) {
                     uint32_t u[16], v[16];                     // outputs 0 to 15 and 16 to 31 of the quarter
                     tmem_ld_16x32(t_addr + r * kRows + c, u);
                     tmem_ld_16x32(t_addr + r * kRows + c + (16u << 16), v);
@@ -341,21 +362,20 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
                             }
                         }
                         // one rounding, then ReLU on the rounded pairs (max with +0 is exact on them)
-                        uint32_t w[4];
+                        uint32_t h[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            w[i] = cvt_bf16x2(f[2 * i], f[2 * i + 1]);
-                            if (p.relu) w[i] = relu_bf16x2(w[i]);
+                            h[i] = cvt_bf16x2(f[2 * i], f[2 * i + 1]);
+                            if (p.relu) h[i] = relu_bf16x2(h[i]);
                         }
                         if (res) __syncwarp();                 // (every lane has read these rows' residuals)
-                        stmatrix_x4_trans(sa, w[0], w[1], w[2], w[3]);
+                        stmatrix_x4_trans(sa, h[0], h[1], h[2], h[3]);
                     }
                 }
                 fence_proxy_async_smem();                      // the TMA store reads what this thread wrote
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bars->slab_done[slot]);
             }
-            n += (uint32_t)(halves * blocks);
             if (!ok) break;
             // this warp has read its part of the accumulator: the MMA warp may overwrite it
             tc_fence_before_sync();
@@ -363,52 +383,43 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
             if (lane == 0) mbar_arrive(&bars->acc_empty[acc]);
         }
     } else if (warp >= R::kFirstEpi) {
-        // ---- epilogue from registers: warp -> lane quarter and a share of the accumulator's columns -------------------------------------
-        const int quarter = warp & 3, part = (warp - R::kFirstEpi) >> 2, share = p.N / (R::kEpiWarps / 4);
+        // ---- epilogue from registers, by the same groups; a lane writes one output of 64 rows of a block ----------------------
+        const int e = warp - R::kFirstEpi, group = e >> 3, quarter = warp & 3, part = (e >> 2) & 1;
         uint32_t it = 0;
-        for (int tile = blockIdx.x; tile < p.n_tiles; tile += gridDim.x, ++it) {
-            const int mt = tile / p.nOT, ot = tile - mt * p.nOT, o = ot * kRows + quarter * 32 + lane;
+        bool ok = true;
+        for (TileWalk w(p); w.in(p) && ok; w.next(p), ++it) {
+            if (p.acc == 2 && R::kGroups == 2 && (it & 1u) != (uint32_t)group) continue;
+            const int o = w.ot * kRows + quarter * 32 + lane, blocks = w.blocks(p);
             const uint32_t acc = p.acc == 2 ? it & 1u : 0u, lap = p.acc == 2 ? it >> 1 : it;
-            const int m0 = mt * p.N + part * share;
-            const int64_t at = (int64_t)m0 * p.O + o + z;
-            const int n = o < p.O ? p.M - m0 : 0;              // rows from m0 on (may be none)
-            const uint32_t t_addr = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * p.N + (uint32_t)(part * share);
             const float b = bias && o < p.O ? __ldg(bias + o + z) : 0.f;
-            // the accumulator is in registers: the MMA warp may overwrite it
-            auto release = [&]() {
-                tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bars->acc_empty[acc]);
-            };
-            uint32_t v[32];
-            if (kMx && p.acc == 1 && !res) {
-                // one accumulator: both batches of the share at once (the residuals' registers are free)
-                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&bars->acc_full[acc], lap & 1u, abort_flag, ws, 0xB500))) break;
+            bool waited = false;
+            for (int r = p.acc == 1 && R::kGroups == 2 ? group : 0; r < blocks && ok; r += p.acc == 1 ? R::kGroups : 1)
+                for (int c = 0; c < 64 && ok; c += 32) {
+                    const int m0 = w.mt * p.N + r * kRows + part * 64 + c, n = o < p.O ? p.M - m0 : 0;       // rows from m0 on (may be none)
+                    const int64_t at = (int64_t)m0 * p.O + o + z;
+                    float add[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) add[i] = b;
+                    if (res) load_residuals<kBf16>(add, b, res, at, p.O, n);
+                    if (!waited) {
+                        ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->acc_full[acc], lap & 1u, abort_flag, ws, 0xB520));
+                        if (!ok) break;
+                        tc_fence_after_sync();
+                        waited = true;
+                    }
+                    uint32_t v[32];
+                    tmem_ld_x32(tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * p.N + (uint32_t)(r * kRows + part * 64 + c), v);
+                    tmem_ld_wait();
+                    store_rows<kBf16>(v, add, y, at, p.O, n, p.relu);
+                }
+            if (ok && !waited) {                               // (no block of this tile is the group's: it hands the accumulator on all the same)
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->acc_full[acc], lap & 1u, abort_flag, ws, 0xB530));
                 tc_fence_after_sync();
-                uint32_t v2[32];
-                tmem_ld_x32(t_addr, v);
-                tmem_ld_x32(t_addr + 32, v2);
-                tmem_ld_wait();
-                release();
-                store_rows<kBf16>(v, b, y, at, p.O, n, p.relu);
-                store_rows<kBf16>(v2, b, y, at + (int64_t)32 * p.O, p.O, n - 32, p.relu);
-                continue;
             }
-            float add[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) add[i] = b;
-            if (res) load_residuals<kBf16>(add, b, res, at, p.O, n);
-            if (!__all_sync(0xFFFFFFFFu, mbar_wait(&bars->acc_full[acc], lap & 1u, abort_flag, ws, 0xB510))) break;
-            tc_fence_after_sync();
-            for (int c = 0; c < share; c += 32) {
-                tmem_ld_x32(t_addr + c, v);
-                tmem_ld_wait();
-                if (c + 32 == share) release();
-                if (c && res) load_residuals<kBf16>(add, b, res, at + (int64_t)c * p.O, p.O, n - c);
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + add[i]);
-                store_rows<kBf16>(v, 0.f, y, at + (int64_t)c * p.O, p.O, n - c, p.relu);
-            }
+            if (!ok) break;
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars->acc_empty[acc]);
         }
     }
     tc_fence_before_sync();
@@ -442,6 +453,8 @@ bool plan(const npas_mx_linear_desc &d, MxPsParams &p, int sms)
     const long long tiles = (long long)p.nMT * p.nOT;
     if (tiles > 0x7FFFFFFF) return false;
     p.n_tiles = (int)tiles;
+    const int grid = p.n_tiles < sms ? p.n_tiles : sms;
+    p.grid = grid; p.step_mt = grid / p.nOT; p.step_ot = grid % p.nOT;
     p.w_scales = LW.off_scales; p.x_scales = LX.off_scales;
     p.x_bytes = (uint32_t)p.N * 128u;
     p.xs_bytes = mx ? (uint32_t)p.N / kRows * kScaleBytes : 0u;
@@ -449,6 +462,7 @@ bool plan(const npas_mx_linear_desc &d, MxPsParams &p, int sms)
     const uint32_t budget = kSmemLimit - (uint32_t)sizeof(MxPsBars) - 128u - 1024u;
     // Slabs for bf16 outputs with rows on 16-byte boundaries: four, eight where residuals are ahead of little else; and the input's ring
     p.NS = p.y_bf16 && d.O % 8 == 0 ? (mx && d.has_residual && p.nS <= 2 && p.N == 128 ? 8 : 4) : 0;
+    p.ns_log = p.NS == 8 ? 3 : 2;
     if (!mx) p.SX = p.N == 256 ? 3 : 6;
     const uint32_t fixed = (uint32_t)p.SX * p.x_bytes + (uint32_t)p.NS * kSlabBytes;
     p.S = (int)((budget - fixed) / p.stage_bytes);
@@ -499,8 +513,7 @@ npas_status linear_mx_ps_launch(const npas_mx_linear_desc &d, const void *x, int
     const auto kernel = mx ? (p.y_bf16 ? linear_mx_ps_kernel<true, true> : linear_mx_ps_kernel<true, false>)
                            : (p.y_bf16 ? linear_mx_ps_kernel<false, true> : linear_mx_ps_kernel<false, false>);
     if (allow_dynamic_smem(reinterpret_cast<const void *>(kernel), (int)kSmemLimit) != NPAS_OK) return NPAS_ERR_CUDA;
-    const int sms = sm_count();
-    const cudaError_t e = launch_pdl(Launch(), kernel, dim3((unsigned)(p.n_tiles < sms ? p.n_tiles : sms)), dim3(mx ? Roles<true>::kThreads : Roles<false>::kThreads),
+    const cudaError_t e = launch_pdl(Launch(), kernel, dim3((unsigned)p.grid), dim3(mx ? Roles<true>::kThreads : Roles<false>::kThreads),
                                      p.smem_bytes, st, tmx, tmw, tmy, tmr, p, static_cast<const uint8_t *>(x), static_cast<const uint8_t *>(w), bias, res, y, ws);
     count_launch();
     return e == cudaSuccess ? launch_status() : NPAS_ERR_CUDA;
