@@ -187,14 +187,15 @@ typedef struct {
  * quantize_x: a bf16 input is quantised on its way in (workspace: npas_linear_mx_workspace), the result is that of
  * npas_quantize_mx and a call on its blob.  path: 0 = automatic, 1 = force the kernel on CUDA cores (fp32; every
  * geometry), 2 = automatic among the tcgen05 kernels, 3 = force the tcgen05 kernel whose 128-row operand are the
- * weights (few rows of X), 4 = force the tcgen05 kernel with persistent tiles (NPAS_ERR_UNSUPPORTED when the geometry is outside the requested kernel's envelope). */
+ * weights (few rows of X), 4 = force the tcgen05 kernel with persistent tiles, 5 = force the
+ * variant of that kernel that runs on CTA pairs (cta_group::2; 4-bit inputs) (NPAS_ERR_UNSUPPORTED when the geometry is outside the requested kernel's envelope). */
 typedef struct {
     int32_t M, I, O;
     int32_t x_dtype, quantize_x, y_dtype;
     int32_t relu, has_bias, has_residual;
     int32_t path;
-    int32_t variant; /* 0 = the planner's choice; path 3: CTAs that share a tile and split the columns (1, 2, 4 or 8); path 4: rows of X in a
-                        tile (128 or 256) */
+    int32_t variant; /* 0 = the planner's choice; path 3: CTAs that share a tile and split the columns (1, 2, 4 or 8); paths 4 and 5: rows of X
+                        in a tile (128 or 256), path 5 + (1 << 16): weights are loaded for every tile */
 } npas_mx_linear_desc;
 
 /* ---- mask helpers (paper Sec. 3: the structural constraint of each scheme) --------------------

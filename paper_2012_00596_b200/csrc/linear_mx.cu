@@ -20,7 +20,7 @@ npas_status check_args(const npas_mx_linear_desc *d)
     return NPAS_OK;
 }
 
-// 1: CUDA cores, 3: few rows, 4: persistent tiles.  0: the requested path does not take the geometry.
+// 1: CUDA cores, 3: few rows, 4: persistent tiles, 5: the same on CTA pairs.  0: the requested path does not take the geometry.
 int kernel_for(const npas_mx_linear_desc &d)
 {
     npas_mx_linear_desc in = d;
@@ -29,9 +29,11 @@ int kernel_for(const npas_mx_linear_desc &d)
         case 1: return d.variant ? 0 : 1;
         case 3: return linear_mx_sw_supported(in) ? 3 : 0;
         case 4: return linear_mx_ps_supported(in) ? 4 : 0;
+        case 5: return linear_mx_d2_supported(in) ? 5 : 0;
         case 0: case 2: break;
         default: return 0;
     }
+    if (d.M > 128 && d.O > 128 && linear_mx_d2_supported(in)) return 5;
     if (d.M > 128 && linear_mx_ps_supported(in)) return 4;
     if (linear_mx_sw_supported(in)) return 3;
     return d.path == 2 ? 0 : 1;
@@ -143,6 +145,7 @@ npas_status npas_internal_linear_mx(const npas_mx_linear_desc *d, const void *x,
     switch (kernel) {
         case 1: return linear_mx_simt_launch(in, x, w, bias, res, y, st);
         case 3: return linear_mx_sw_launch(in, x, pitch, w, bias, res, y, static_cast<uint32_t *>(ws), st);
+        case 5: return linear_mx_d2_launch(in, x, w, bias, res, y, static_cast<uint32_t *>(ws), st);
         case 4: return linear_mx_ps_launch(in, x, pitch, w, bias, res, y, static_cast<uint32_t *>(ws), st);
     }
     return NPAS_ERR_UNSUPPORTED;

@@ -30,6 +30,17 @@ __device__ __forceinline__ void mma_mxf4_ss(uint32_t d_tmem, uint64_t a_desc, ui
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa_tmem), "r"(sb_tmem), "r"(accumulate) : "memory");
 }
 
+// The same shared by the two CTAs of a cluster: A 128 rows per CTA, B N/2 rows per CTA, scales of A per CTA, of B in both; ONE thread of the leader.
+__device__ __forceinline__ void mma_mxf4_ss_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa_tmem, uint32_t sb_tmem,
+                                                 uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa_tmem), "r"(sb_tmem), "r"(accumulate) : "memory");
+}
+
 // D[tmem] (+)= A[tmem: bf16 pairs, 128 lanes x 8 columns] * B[smem]; issued by ONE thread.
 __device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
 {
@@ -46,6 +57,13 @@ __device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t saddr)
 {
     const uint64_t desc = smem_desc_kmajor(saddr, 16, 128);
     asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+
+// the same in both CTAs of a pair, each from its own shared memory
+__device__ __forceinline__ void copy_scales_pair(uint32_t tmem, uint32_t saddr)
+{
+    const uint64_t desc = smem_desc_kmajor(saddr, 16, 128);
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
 
 // 32 consecutive 32-bit columns of the warp's lane quarter (thread i writes TMEM lane base + i).
@@ -145,6 +163,16 @@ inline bool mx_encode_values(CUtensorMap *map, const void *blob, const MxLayout 
     const cuuint32_t box[2] = {128, box_rows}, estr[2] = {1, 1};
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(static_cast<const uint8_t *>(blob)) + L.off_values, dims, strides, box, estr,
                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// tiles of scales as rows of 128 words: boxes of two (a stage of 256 columns)
+inline bool mx_encode_scales(CUtensorMap *map, const void *blob, const MxLayout &L)
+{
+    EncodeTiledFn enc = encode_tiled_fn();
+    if (!enc) return false;
+    const cuuint64_t dims[2] = {kMxScaleTile / 4, (cuuint64_t)L.nRT * L.nKT}, strides[1] = {kMxScaleTile};
+    const cuuint32_t box[2] = {kMxScaleTile / 4, 2}, estr[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<uint8_t *>(static_cast<const uint8_t *>(blob)) + L.off_scales, dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // a bf16 matrix with rows of `pitch` elements (a multiple of 8; inputs, outputs, residuals): boxes of 64 columns x rows, 128-byte swizzled, past the end zeros
 inline bool mx_encode_bf16(CUtensorMap *map, const void *base, uint64_t cols, uint64_t pitch, uint64_t rows, uint32_t box_rows)
