@@ -59,11 +59,11 @@ __device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t saddr)
     asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
 
-// the same in both CTAs of a pair, each from its own shared memory
-__device__ __forceinline__ void copy_scales_pair(uint32_t tmem, uint32_t saddr)
+// eight columns of the warp's lane quarter
+__device__ __forceinline__ void tmem_st_x8(uint32_t taddr, const uint4 &a, const uint4 &b)
 {
-    const uint64_t desc = smem_desc_kmajor(saddr, 16, 128);
-    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"r"(taddr), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
 }
 
 // 32 consecutive 32-bit columns of the warp's lane quarter (thread i writes TMEM lane base + i).
@@ -163,16 +163,6 @@ inline bool mx_encode_values(CUtensorMap *map, const void *blob, const MxLayout 
     const cuuint32_t box[2] = {128, box_rows}, estr[2] = {1, 1};
     return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(static_cast<const uint8_t *>(blob)) + L.off_values, dims, strides, box, estr,
                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-// tiles of scales as rows of 128 words: boxes of two (a stage of 256 columns)
-inline bool mx_encode_scales(CUtensorMap *map, const void *blob, const MxLayout &L)
-{
-    EncodeTiledFn enc = encode_tiled_fn();
-    if (!enc) return false;
-    const cuuint64_t dims[2] = {kMxScaleTile / 4, (cuuint64_t)L.nRT * L.nKT}, strides[1] = {kMxScaleTile};
-    const cuuint32_t box[2] = {kMxScaleTile / 4, 2}, estr[2] = {1, 1};
-    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<uint8_t *>(static_cast<const uint8_t *>(blob)) + L.off_scales, dims, strides, box, estr,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // a bf16 matrix with rows of `pitch` elements (a multiple of 8; inputs, outputs, residuals): boxes of 64 columns x rows, 128-byte swizzled, past the end zeros
 inline bool mx_encode_bf16(CUtensorMap *map, const void *base, uint64_t cols, uint64_t pitch, uint64_t rows, uint32_t box_rows)
