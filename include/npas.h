@@ -194,8 +194,8 @@ typedef struct {
     int32_t x_dtype, quantize_x, y_dtype;
     int32_t relu, has_bias, has_residual;
     int32_t path;
-    int32_t variant; /* 0 = the planner's choice; path 3: CTAs that share a tile and split the columns (1, 2, 4 or 8); paths 4 and 5: rows of X
-                        in a tile (128 or 256), path 5 + (1 << 16): weights are loaded for every tile */
+    int32_t variant; /* 0 = the planner's choice; path 3: CTAs that share a tile and split the columns (1, 2, 4 or 8); path 4: rows of X in a
+                        tile (128 or 256), + (1 << 16): weights are loaded for every tile */
 } npas_mx_linear_desc;
 
 /* ---- mask helpers (paper Sec. 3: the structural constraint of each scheme) --------------------

@@ -3,10 +3,9 @@
 // The kernel of linear_mx_ps.cu for inputs that are blobs, with every MMA shared by the two CTAs of a cluster: each CTA has the weights
 // of its own 128 outputs and one half of the input's rows.  A stage of 256 columns is 32 KB per SM instead of 48 with 256 rows: by
 // themselves the loads of 8192^3 take 230 us on single CTAs (what the SMs take in from L2), the MMAs 120.  Scales go to tensor memory through
-// the registers of four warps per CTA, a lane quarter each, in groups of four stages: tcgen05.cp on a pair takes 130 cycles for 512
+// the registers of four warps per CTA, a lane quarter each, in groups of five stages: tcgen05.cp on a pair takes 130 cycles for 512
 // bytes and holds up the MMAs behind it (8192^3 261 us with six a stage, 177 with none), and a hand-over between the CTAs per stage
-// takes longer than the stage (620).  Where the weights of a tile fit and a pair's tiles all have the same outputs (the number of pairs is a multiple of the
-// tiles across), they are loaded once and stay.  Copies of both CTAs complete on the leader's barriers, the leader's warp 1 issues the
+// takes longer than the stage (620).  Copies of both CTAs complete on the leader's barriers, the leader's warp 1 issues the
 // MMAs and the copies of scales for both and frees stages and hands over accumulators with multicast commits; both CTAs' epilogues
 // (mx_epi.cuh) read their own 128 lanes; the peer's hand the accumulator back through one arrival with release semantics at cluster
 // scope by its warp 1, as in linear_d2.cu.  Every wait is bounded; a role that gives up raises the abort flag of both CTAs.
@@ -26,7 +25,7 @@ constexpr int kMaxStages = 8;
 constexpr int kStoreWarp = 2, kScaleCopyWarp = 3, kFirstScale = 4, kFirstEpi = 8, kEpiWarps = 8, kThreads = (kFirstEpi + kEpiWarps) * 32;
 constexpr uint32_t kSmemLimit = 232448;
 constexpr uint32_t kWBytes = kRows * 128;
-constexpr int kGroup = 4;                                  // stages whose scales are handed over together
+constexpr int kGroup = 5;                                  // stages whose scales are handed over together
 constexpr uint32_t kGroupScales = kGroup * 2 * kMxScaleTile; // bytes of them for 128 rows
 constexpr int kN = 256;                                    // rows of X in a tile
 constexpr uint32_t kXBytes = kN / 2 * 128, kStageBytes = kXBytes + kWBytes;
@@ -233,7 +232,7 @@ linear_mx_d2_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
             if (lane == 0) mbar_arrive(rank == 0 ? &bars->epi.acc_empty[acc] : &bars->acc_done);
         };
         if (kBf16 && p.t.NS)
-            mx_epilogue_slabs<1>(p.t, pair, (int)rank, warp - kFirstEpi, lane, warp & 3, smem_u32(smem), tmem_base, &bars->epi, bias, res != nullptr, abort_flag, ws, release);
+            mx_epilogue_slabs<1, true>(p.t, pair, (int)rank, warp - kFirstEpi, lane, warp & 3, smem_u32(smem), tmem_base, &bars->epi, bias, res != nullptr, abort_flag, ws, release);
         else
             mx_epilogue_rows<1, kBf16>(p.t, pair, (int)rank, warp - kFirstEpi, lane, warp & 3, tmem_base, &bars->epi, bias, res, y, abort_flag, ws, release);
     }

@@ -5,6 +5,8 @@
 // 16-bit input the widening of the weights into tensor memory, and the epilogue are roles of their own that hand stages, slots and
 // accumulators on through barriers, so the next tile is loaded and multiplied while one is written out.  Two accumulators of 128 columns,
 // or one of 256 (with 256 rows of X a weight is fetched half as often, which long inputs need).
+// Where the tiles of a CTA all have the same outputs (the grid is a multiple of the tiles across) and their weights fit, the weights stay: a
+// 4-bit input's in shared memory (their copies were half of a small tile's), a 16-bit input's widened in tensor memory.
 // Outputs leave by mx_epi.cuh.  Every wait is bounded.
 #include "mx_epi.cuh"
 
@@ -16,10 +18,11 @@ namespace {
 
 constexpr int kRows = 128;
 constexpr int kStepCols = 256;                             // columns of a weight stage
-constexpr int kMaxStages = 6, kMaxXStages = 8, kSlots = 4;
+constexpr int kMaxStages = 6, kMaxXStages = 8, kSlots = 4, kMaxSlots = 8;
 constexpr uint32_t kSmemLimit = 232448;
 constexpr uint32_t kWBytes = kRows * 128;
 constexpr uint32_t kScaleBytes = 2 * kMxScaleTile;         // of 128 rows and a stage
+constexpr uint32_t kWStage = kWBytes + kScaleBytes;
 
 // warps: 0 copies, 1 MMAs, then a 16-bit input's own copies and the widening warps, then the epilogue, one of them for the slabs' copies
 template <bool kMx> struct Roles {
@@ -32,8 +35,8 @@ template <bool kMx> struct Roles {
 
 struct MxPsParams {
     MxTiles t;
-    int I, nS, nKT, S, SX;                                     // SX: stages of the input (16 bits)
-    uint32_t x_bytes, xs_bytes, stage_bytes, off_x, off_bar, smem_bytes, tmem_cols, tmem_scales, scale_cols;
+    int I, nS, nKT, S, SX, slots, resident;                    // SX: stages of the input (16 bits); slots: of widened weights; resident: weights stay
+    uint32_t x_bytes, xs_bytes, stage_bytes, x_in_stage, off_stages, off_x, off_bar, smem_bytes, tmem_cols, tmem_scales, scale_cols;
     uint64_t w_scales, x_scales;                           // offsets of the scales in the blobs
     int y_bf16;
 };
@@ -41,7 +44,8 @@ struct MxPsParams {
 struct MxPsBars {
     uint64_t full[kMaxStages], empty[kMaxStages];
     uint64_t x_full[kMaxXStages], x_empty[kMaxXStages];
-    uint64_t slot_full[kSlots], slot_empty[kSlots];
+    uint64_t slot_full[kMaxSlots], slot_empty[kMaxSlots];
+    uint64_t w_full;                                       // resident weights of a 4-bit input
     MxEpiBars epi;
     uint32_t tmem_base;
     uint32_t abort_flag;
@@ -64,7 +68,8 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
     if (tid == 0) {
         for (int s = 0; s < p.S; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], kMx ? 1 : R::kWideWarps); }
         for (int s = 0; s < p.SX; ++s) { mbar_init(&bars->x_full[s], 1); mbar_init(&bars->x_empty[s], 1); }
-        for (int s = 0; s < kSlots; ++s) { mbar_init(&bars->slot_full[s], 4); mbar_init(&bars->slot_empty[s], 1); }
+        for (int s = 0; s < p.slots; ++s) { mbar_init(&bars->slot_full[s], 4); mbar_init(&bars->slot_empty[s], 1); }
+        mbar_init(&bars->w_full, 1);
         mx_epi_init(&bars->epi, p.t, p.t.acc == 2 ? 8 : R::kEpiWarps);
         bars->abort_flag = 0;
         fence_barrier_init();
@@ -83,24 +88,35 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
 
     if (warp == 0) {
         if (lane == 0) {
+            auto scale_bytes = [&](int step) { return (uint32_t)min(2, p.nKT - 2 * step) * kMxScaleTile; };      // (the last tile of columns may stand alone)
+            auto weights = [&](uint8_t *st, uint64_t *bar, int ot, int step) {
+                tma_load_2d(st, &tmap_w, bar, step * 128, ot * kRows);
+                bulk_load_1d(st + kWBytes, wblob + p.w_scales + ((uint64_t)ot * p.nKT + 2 * step) * kMxScaleTile, scale_bytes(step), bar);
+            };
+            MxWalk w(p.t, blockIdx.x, 0);
+            if (kMx && p.resident) {
+                uint32_t bytes = 0;
+                for (int step = 0; step < p.nS; ++step) bytes += kWBytes + scale_bytes(step);
+                mbar_arrive_expect_tx(&bars->w_full, bytes);
+                for (int step = 0; step < p.nS; ++step) weights(smem + (size_t)step * kWStage, &bars->w_full, w.ot, step);
+            }
             uint32_t s = 0, lap = 0;
             bool ok = true;
-            for (MxWalk w(p.t, blockIdx.x, 0); w.in(p.t) && ok; w.next(p.t)) {
-                const int mt = w.mt, ot = w.ot;
+            // (resident weights of a 16-bit input: the first tile's are all there is to load)
+            for (; w.in(p.t) && ok && (kMx || !p.resident || w.tile == (int)blockIdx.x); w.next(p.t)) {
                 for (int step = 0; step < p.nS; ++step) {
                     if (lap >= 1 && !mbar_wait(&bars->empty[s], (lap & 1u) ^ 1u, abort_flag, ws, 0xB100)) { ok = false; break; }
-                    uint8_t *st = smem + (size_t)s * p.stage_bytes;
-                    const uint32_t sb = (uint32_t)min(2, p.nKT - 2 * step) * kMxScaleTile;   // (the last tile of columns may stand alone)
+                    uint8_t *st = smem + p.off_stages + (size_t)s * p.stage_bytes;
+                    const uint32_t sb = scale_bytes(step);
                     // row tiles of X's scales: those that exist
-                    const int xt = kMx ? min(p.t.N / kRows, (p.t.M + kRows - 1) / kRows - mt * (p.t.N / kRows)) : 0;
-                    mbar_arrive_expect_tx(&bars->full[s], kWBytes + sb + (kMx ? p.x_bytes + xt * sb : 0u));
-                    tma_load_2d(st, &tmap_w, &bars->full[s], step * 128, ot * kRows);
-                    bulk_load_1d(st + kWBytes, wblob + p.w_scales + ((uint64_t)ot * p.nKT + 2 * step) * kMxScaleTile, sb, &bars->full[s]);
+                    const int xt = kMx ? min(p.t.N / kRows, (p.t.M + kRows - 1) / kRows - w.mt * (p.t.N / kRows)) : 0;
+                    mbar_arrive_expect_tx(&bars->full[s], (kMx && p.resident ? 0u : kWBytes + sb) + (kMx ? p.x_bytes + xt * sb : 0u));
+                    if (!(kMx && p.resident)) weights(st, &bars->full[s], w.ot, step);
                     if (kMx) {
-                        tma_load_2d(st + kWBytes + kScaleBytes + p.xs_bytes, &tmap_x, &bars->full[s], step * 128, mt * p.t.N);
+                        tma_load_2d(st + p.x_in_stage + p.xs_bytes, &tmap_x, &bars->full[s], step * 128, w.m0(p.t));
                         for (int t = 0; t < xt; ++t)
-                            bulk_load_1d(st + kWBytes + kScaleBytes + t * kScaleBytes,
-                                         xblob + p.x_scales + ((uint64_t)(mt * (p.t.N / kRows) + t) * p.nKT + 2 * step) * kMxScaleTile, sb, &bars->full[s]);
+                            bulk_load_1d(st + p.x_in_stage + t * kScaleBytes,
+                                         xblob + p.x_scales + ((uint64_t)(w.mt * (p.t.N / kRows) + t) * p.nKT + 2 * step) * kMxScaleTile, sb, &bars->full[s]);
                     }
                     if (++s == (uint32_t)p.S) { s = 0; ++lap; }
                 }
@@ -109,8 +125,16 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
     } else if (warp == 1) {
         if (elect_one()) {
             const uint32_t base = smem_u32(smem) & 0x3FFFFu;
-            uint32_t s = 0, ph = 0, it = 0, k_all = 0;
+            uint32_t s = 0, ph = 0, it = 0, slot = 0, slot_ph = 0;
             bool ok = true;
+            // tensor memory of scales: two tiles of W's a stage (a step where they stay), then X's, a K tile's row tiles side by side
+            const uint32_t xc = (uint32_t)p.t.N / 32, w_cols = kMx && p.resident ? 8u * p.nS : 0u;
+            if (kMx && p.resident) {
+                ok = mbar_wait(&bars->w_full, 0, abort_flag, ws, 0xB330);
+                for (int step = 0; step < p.nS && ok; ++step)
+                    for (int t = 0; t < 2 && 2 * step + t < p.nKT; ++t)
+                        copy_scales(tmem_base + p.tmem_scales + 8 * step + 4 * t, base + step * kWStage + kWBytes + t * kMxScaleTile);
+            }
             for (int tile = blockIdx.x; tile < p.t.n_tiles && ok; tile += p.t.grid, ++it) {
                 const uint32_t acc = p.t.acc == 2 ? it & 1u : 0u, lap_acc = p.t.acc == 2 ? it >> 1 : it;
                 if (lap_acc >= 1 && !mbar_wait(&bars->epi.acc_empty[acc], (lap_acc & 1u) ^ 1u, abort_flag, ws, 0xB200)) break;
@@ -120,35 +144,35 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
                     for (int step = 0; step < p.nS; ++step) {
                         if (!mbar_wait(&bars->full[s], ph, abort_flag, ws, 0xB300)) { ok = false; break; }
                         tc_fence_after_sync();
-                        const uint32_t st = base + s * p.stage_bytes, a_lo = (st >> 4) | kMxDescLboOne;
-                        const uint32_t b_lo = ((st + kWBytes + kScaleBytes + p.xs_bytes) >> 4) | kMxDescLboOne;
-                        // tensor memory of this stage's scales: two tiles of W's, then X's, a K tile's row tiles side by side
-                        const uint32_t sf = tmem_base + p.tmem_scales + s * p.scale_cols, xc = (uint32_t)p.t.N / 32;
+                        const uint32_t st = base + p.off_stages + s * p.stage_bytes, wst = p.resident ? base + step * kWStage : st, xs = st + p.x_in_stage;
+                        const uint32_t a_lo = (wst >> 4) | kMxDescLboOne, b_lo = ((xs + p.xs_bytes) >> 4) | kMxDescLboOne;
+                        const uint32_t sx = tmem_base + p.tmem_scales + w_cols + s * p.scale_cols + (p.resident ? 0u : 8u);
+                        const uint32_t sw = p.resident ? tmem_base + p.tmem_scales + 8 * step : sx - 8u;
                         const int n = min(4, nK - 4 * step);
                         for (int t = 0; t < (n + 1) / 2; ++t) {
-                            copy_scales(sf + 4 * t, st + kWBytes + t * kMxScaleTile);
-                            for (int r = 0; r < p.t.N / kRows; ++r)
-                                copy_scales(sf + 8 + xc * t + 4 * r, st + kWBytes + kScaleBytes + r * kScaleBytes + t * kMxScaleTile);
+                            if (!p.resident) copy_scales(sw + 4 * t, wst + kWBytes + t * kMxScaleTile);
+                            for (int r = 0; r < p.t.N / kRows; ++r) copy_scales(sx + xc * t + 4 * r, xs + r * kScaleBytes + t * kMxScaleTile);
                         }
                         for (int j = 0; j < n; ++j)                                  // 64 columns = 32 bytes inside the swizzled row
                             mma_mxf4_ss(d_tmem, mx_desc64(a_lo + 2 * j), mx_desc64(b_lo + 2 * j), idesc_mxf4(128, (uint32_t)p.t.N, j & 1),
-                                        sf + 4 * (j / 2), sf + 8 + xc * (j / 2), step > 0 || j > 0);
+                                        sw + 4 * (j / 2), sx + xc * (j / 2), step > 0 || j > 0);
                         mma_commit(&bars->empty[s]);
                         if (++s == (uint32_t)p.S) { s = 0; ph ^= 1u; }
                     }
                 } else {
                     const uint32_t idesc = idesc_bf16_f32(128, (uint32_t)p.t.N), xb = base + p.off_x;
-                    for (int k = 0; k < nK; ++k, ++k_all) {
-                        const uint32_t slot = k_all % kSlots;
+                    for (int k = 0; k < nK; ++k) {
+                        // (weights that stay are waited for once: slot k holds step k)
                         if (!mbar_wait(&bars->x_full[s], ph, abort_flag, ws, 0xB310) ||
-                            !mbar_wait(&bars->slot_full[slot], (k_all / kSlots) & 1u, abort_flag, ws, 0xB320)) { ok = false; break; }
+                            (!(p.resident && it > 0) && !mbar_wait(&bars->slot_full[slot], slot_ph, abort_flag, ws, 0xB320))) { ok = false; break; }
                         tc_fence_after_sync();
                         const uint32_t b_lo = ((xb + s * p.x_bytes) >> 4) | kMxDescLboOne, a_t = tmem_base + p.tmem_scales + slot * 32u;
 #pragma unroll
                         for (uint32_t j = 0; j < 4; ++j)
                             mma_bf16_ts(d_tmem, a_t + 8 * j, mx_desc64(b_lo + 2 * j), idesc, (k > 0 || j > 0) ? 1u : 0u);
-                        mma_commit(&bars->slot_empty[slot]);
+                        if (!p.resident) mma_commit(&bars->slot_empty[slot]);
                         mma_commit(&bars->x_empty[s]);
+                        if (++slot == (uint32_t)(p.resident ? nK : p.slots)) { slot = 0; slot_ph ^= 1u; }
                         if (++s == (uint32_t)p.SX) { s = 0; ph ^= 1u; }
                     }
                 }
@@ -173,20 +197,20 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
         const int group = (warp - R::kFirstWide) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
         bool ok = true;
         uint32_t s = 0, ph = 0, k0 = 0;                        // k0: K steps before this stage
-        for (int tile = blockIdx.x; tile < p.t.n_tiles && ok; tile += p.t.grid) {
+        for (int tile = blockIdx.x; tile < p.t.n_tiles && ok && !(p.resident && tile != (int)blockIdx.x); tile += p.t.grid) {
             for (int step = 0; step < p.nS && ok; ++step) {
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->full[s], ph, abort_flag, ws, 0xB400));
                 if (!ok) break;
                 const uint8_t *st = smem + (size_t)s * p.stage_bytes;
                 const int n = min(4, nK - 4 * step);
                 for (int q = (int)((group ^ k0) & 1u); q < n; q += 2) {
-                    const uint32_t k = k0 + q, slot = k % kSlots;
+                    const uint32_t k = k0 + q, slot = p.resident ? k : k % kSlots;
                     const uint4 a = *reinterpret_cast<const uint4 *>(st + r * 128 + ((2 * q) ^ (r & 7)) * 16);
                     const uint4 b = *reinterpret_cast<const uint4 *>(st + r * 128 + ((2 * q + 1) ^ (r & 7)) * 16);
                     const uint32_t codes = *reinterpret_cast<const uint32_t *>(st + kWBytes + (q >> 1) * kMxScaleTile + lane * 16 + quarter * 4) >> (16 * (q & 1));
                     uint32_t v[32];
                     mx_widen(v, a, b, codes & 255u, (codes >> 8) & 255u);
-                    if (k >= kSlots) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->slot_empty[slot], ((k / kSlots) & 1u) ^ 1u, abort_flag, ws, 0xB410));
+                    if (!p.resident && k >= kSlots) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->slot_empty[slot], ((k / kSlots) & 1u) ^ 1u, abort_flag, ws, 0xB410));
                     if (!ok) break;
                     tc_fence_after_sync();
                     tmem_st_x32(tmem_base + ((uint32_t)(quarter * 32) << 16) + p.tmem_scales + slot * 32u, v);
@@ -210,7 +234,7 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
             if (lane == 0) mbar_arrive(&bars->epi.acc_empty[acc]);
         };
         if (kBf16 && p.t.NS)
-            mx_epilogue_slabs<R::kGroups>(p.t, blockIdx.x, 0, warp - R::kFirstEpi, lane, warp & 3, smem_u32(smem), tmem_base, &bars->epi, bias, res != nullptr, abort_flag,
+            mx_epilogue_slabs<R::kGroups, false>(p.t, blockIdx.x, 0, warp - R::kFirstEpi, lane, warp & 3, smem_u32(smem), tmem_base, &bars->epi, bias, res != nullptr, abort_flag,
                                           ws, release);
         else
             mx_epilogue_rows<R::kGroups, kBf16>(p.t, blockIdx.x, 0, warp - R::kFirstEpi, lane, warp & 3, tmem_base, &bars->epi, bias, res, y, abort_flag, ws, release);
@@ -238,32 +262,41 @@ bool plan(const npas_mx_linear_desc &d, MxPsParams &p, int sms)
     p.y_bf16 = d.y_dtype == NPAS_BF16;
     p.nS = (d.I + kStepCols - 1) / kStepCols;
     p.nKT = (int)LW.nKT;
-    const int N = d.variant ? d.variant : (d.I >= 2048 && (long long)((d.M + 255) / 256) * ((d.O + 127) / 128) >= sms ? 256 : 128);
-    if (N != 128 && N != 256) return false;
+    const int want = d.variant & 0xFFFF;
+    const int N = want ? want : d.I >= 2048 && (long long)((d.M + 255) / 256) * ((d.O + 127) / 128) >= sms ? 256 : 128;
+    if ((N != 128 && N != 256) || d.variant >> 17) return false;
     mx_tiles_plan(p.t, d, N, kRows, N == 128 ? 2 : 1, sms);
     if (!p.t.n_tiles) return false;
+    // Weights that stay: with more than a round of tiles, and few SMs idle for a grid that is a multiple of the tiles across
+    const int same = sms / p.t.n_ot * p.t.n_ot, nK = (d.I + 63) / 64;
+    p.resident = !(d.variant >> 16) && p.t.n_tiles > sms && same * 8 >= sms * 7 && (mx ? p.nS <= 4 : nK <= kMaxSlots);
+    if (p.resident) mx_tiles_plan(p.t, d, N, kRows, p.t.acc, same);
     p.w_scales = LW.off_scales; p.x_scales = LX.off_scales;
     p.x_bytes = (uint32_t)N * 128u;
     p.xs_bytes = mx ? (uint32_t)N / kRows * kScaleBytes : 0u;
-    p.stage_bytes = round_up(kWBytes + kScaleBytes + (mx ? p.xs_bytes + p.x_bytes : 0u), 1024);
+    p.x_in_stage = mx && p.resident ? 0u : kWStage;
+    p.off_stages = mx && p.resident ? (uint32_t)p.nS * kWStage : 0u;
+    p.stage_bytes = p.x_in_stage + (mx ? p.xs_bytes + p.x_bytes : 0u);
     const uint32_t budget = kSmemLimit - (uint32_t)sizeof(MxPsBars) - 128u - 1024u;
     // Slabs for bf16 outputs with rows on 16-byte boundaries: two where the loads need the room (256 rows of X), else four, eight where
     // residuals are ahead of little else; and the input's ring
     p.t.NS = !p.y_bf16 || d.O % 8 ? 0 : N == 256 && p.nS > 2 ? 2 : mx && d.has_residual && p.nS <= 2 && N == 128 ? 8 : 4;
     while ((1 << p.t.ns_log) < p.t.NS) ++p.t.ns_log;
+    p.slots = mx ? 0 : p.resident ? nK : kSlots;
     if (!mx) p.SX = N == 256 ? (p.t.NS == 4 ? 3 : 4) : 6;
-    const uint32_t fixed = (uint32_t)p.SX * p.x_bytes + (uint32_t)p.t.NS * kMxSlabBytes;
+    const uint32_t fixed = p.off_stages + (uint32_t)p.SX * p.x_bytes + (uint32_t)p.t.NS * kMxSlabBytes;
+    if (fixed >= budget) return false;
     p.S = (int)((budget - fixed) / p.stage_bytes);
     if (p.S > kMaxStages) p.S = kMaxStages;
     if (p.S < 2) return false;
-    p.off_x = (uint32_t)p.S * p.stage_bytes;
+    p.off_x = p.off_stages + (uint32_t)p.S * p.stage_bytes;
     p.t.off_slabs = p.off_x + (uint32_t)p.SX * p.x_bytes;
     p.off_bar = round_up(p.t.off_slabs + (uint32_t)p.t.NS * kMxSlabBytes, 128);
     p.smem_bytes = p.off_bar + (uint32_t)sizeof(MxPsBars) + 1024u;
     if (p.smem_bytes > kSmemLimit) return false;
     p.tmem_scales = 256;
-    p.scale_cols = 8 + 2 * (uint32_t)N / 32;
-    const uint32_t cols = p.tmem_scales + (mx ? p.scale_cols * p.S : 32u * kSlots);
+    p.scale_cols = (p.resident ? 0 : 8) + 2 * (uint32_t)N / 32;
+    const uint32_t cols = p.tmem_scales + (mx ? (p.resident ? 8u * p.nS : 0u) + p.scale_cols * p.S : 32u * p.slots);
     p.tmem_cols = 32;
     while (p.tmem_cols < cols) p.tmem_cols *= 2;
     return p.tmem_cols <= 512;

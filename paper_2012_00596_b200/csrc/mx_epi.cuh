@@ -104,8 +104,10 @@ __device__ __forceinline__ void mx_slab_copies(const MxTiles &p, int unit, int r
     bulk_wait_read<0>();                                       // the slabs stay valid until the last store has read them
 }
 
-// ---- epilogue through slabs; e: number of the warp among the epilogue's, `release(acc)`: this warp has the sums in registers ---------------
-template <int kGroups, typename F>
+// ---- epilogue through slabs; e: number of the warp among the epilogue's, `release(acc)`: this warp has the sums in registers.  kBoth: a warp
+// with both blocks of a tile of 256 rows rounds the first one's sums, takes the second one's and hands the accumulator back before it waits
+// for a slab (without residuals; 32 more registers) -------------------------------------------------------------------------------
+template <int kGroups, bool kBoth, typename F>
 __device__ __forceinline__ void mx_epilogue_slabs(const MxTiles &p, int unit, int rank, int e, int lane, int quarter, uint32_t smem, uint32_t tmem_base, MxEpiBars *bars,
                                                   const float *bias, bool res, volatile uint32_t *abort_flag, uint32_t *ws, F release)
 {
@@ -127,51 +129,84 @@ __device__ __forceinline__ void mx_epilogue_slabs(const MxTiles &p, int unit, in
         if (!__all_sync(0xFFFFFFFFu, mbar_wait(&bars->acc_full[acc], lap & 1u, abort_flag, ws, 0xC500))) return;
         tc_fence_after_sync();
         const uint32_t t_addr = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * p.N + (uint32_t)(part * 64);
-        int r = p.acc == 1 && kGroups == 2 ? group : 0;
-        bool held = true;
-        for (; r < blocks && half < halves; r += step) {
-            uint32_t u[2][16], v[2][16];                       // outputs 0 to 15 and 16 to 31 of the quarter, 32 rows each
+        // outputs 0 to 15 and 16 to 31 of the quarter, twice 32 rows of block r
+        auto take = [&](int r, uint32_t (&u)[2][16], uint32_t (&v)[2][16]) {
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 tmem_ld_16x32(t_addr + r * 128 + c * 32, u[c]);
                 tmem_ld_16x32(t_addr + r * 128 + c * 32 + (16u << 16), v[c]);
             }
             tmem_ld_wait();
-            if (r + step >= blocks) { release(acc); held = false; }
-            const uint32_t at = n_tile + (uint32_t)(r * halves + half), slot = at & (p.NS - 1), slab = lane_at + slot * kMxSlabBytes, use = at >> p.ns_log;
-            // with residuals: they have landed; without: the store that last used the slab has read it (from its second use on)
-            if (res || use)
-                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&bars->slab_ready[slot], (res ? use : use - 1) & 1u, abort_flag, ws, 0xC510))) return;
+        };
+        // eight rows of Y, k of 32: + bias (+ residuals q), one rounding, then ReLU on the rounded pairs (max with +0 is exact on them)
+        auto rounded = [&](const uint32_t (&u)[16], const uint32_t (&v)[16], int k, const uint32_t (&q)[4], uint32_t (&h)[4]) {
+            float f[8] = {__uint_as_float(u[4 * k]) + b[0], __uint_as_float(u[4 * k + 1]) + b[0], __uint_as_float(u[4 * k + 2]) + b[1],
+                          __uint_as_float(u[4 * k + 3]) + b[1], __uint_as_float(v[4 * k]) + b[2], __uint_as_float(v[4 * k + 1]) + b[2],
+                          __uint_as_float(v[4 * k + 2]) + b[3], __uint_as_float(v[4 * k + 3]) + b[3]};
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {                  // eight rows of Y
-                    float f[8] = {__uint_as_float(u[c][4 * k]) + b[0], __uint_as_float(u[c][4 * k + 1]) + b[0], __uint_as_float(u[c][4 * k + 2]) + b[1],
-                                  __uint_as_float(u[c][4 * k + 3]) + b[1], __uint_as_float(v[c][4 * k]) + b[2], __uint_as_float(v[c][4 * k + 1]) + b[2],
-                                  __uint_as_float(v[c][4 * k + 2]) + b[3], __uint_as_float(v[c][4 * k + 3]) + b[3]};
-                    const uint32_t sa = slab + (uint32_t)(c * 32 + 8 * k) * 128u;
-                    if (res) {
-                        uint32_t q[4];
-                        ldmatrix_x4_trans(sa, q);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            f[2 * i] += __uint_as_float(q[i] << 16);
-                            f[2 * i + 1] += __uint_as_float(q[i] & 0xFFFF0000u);
-                        }
-                    }
-                    // one rounding, then ReLU on the rounded pairs (max with +0 is exact on them)
-                    uint32_t h[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        h[i] = cvt_bf16x2(f[2 * i], f[2 * i + 1]);
-                        if (p.relu) h[i] = relu_bf16x2(h[i]);
-                    }
-                    if (res) __syncwarp();                     // (every lane has read these rows' residuals)
-                    stmatrix_x4_trans(sa, h[0], h[1], h[2], h[3]);
+            for (int i = 0; i < 4; ++i) {
+                if (res) {
+                    f[2 * i] += __uint_as_float(q[i] << 16);
+                    f[2 * i + 1] += __uint_as_float(q[i] & 0xFFFF0000u);
                 }
+                h[i] = cvt_bf16x2(f[2 * i], f[2 * i + 1]);
+                if (p.relu) h[i] = relu_bf16x2(h[i]);
+            }
+        };
+        // the slab of block r, ready for this warp.  With residuals: they have landed; without: the store that last used the slab has read
+        // it (from its second use on)
+        auto slab_of = [&](int r, uint32_t &slot) {
+            const uint32_t at = n_tile + (uint32_t)(r * halves + half), use = at >> p.ns_log;
+            slot = at & (p.NS - 1);
+            return !(res || use) || __all_sync(0xFFFFFFFFu, mbar_wait(&bars->slab_ready[slot], (res ? use : use - 1) & 1u, abort_flag, ws, 0xC510));
+        };
+        auto hand_over = [&](uint32_t slot) {
             fence_proxy_async_smem();                          // the TMA store reads what this thread wrote
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars->slab_done[slot]);
+        };
+        constexpr uint32_t kNone[4] = {0, 0, 0, 0};
+        uint32_t slot;
+        if (kBoth && !res && blocks == 2 && half < halves) {
+            uint32_t h[8][4];
+            {
+                uint32_t u[2][16], v[2][16];
+                take(0, u, v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) rounded(u[k >> 2], v[k >> 2], k & 3, kNone, h[k]);
+            }
+            uint32_t u[2][16], v[2][16];
+            take(1, u, v);
+            release(acc);
+            if (!slab_of(0, slot)) return;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) stmatrix_x4_trans(lane_at + slot * kMxSlabBytes + (uint32_t)k * 1024u, h[k][0], h[k][1], h[k][2], h[k][3]);
+            hand_over(slot);
+            if (!slab_of(1, slot)) return;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                rounded(u[k >> 2], v[k >> 2], k & 3, kNone, h[0]);
+                stmatrix_x4_trans(lane_at + slot * kMxSlabBytes + (uint32_t)k * 1024u, h[0][0], h[0][1], h[0][2], h[0][3]);
+            }
+            hand_over(slot);
+            continue;
+        }
+        bool held = true;
+        for (int r = p.acc == 1 && kGroups == 2 ? group : 0; r < blocks && half < halves; r += step) {
+            uint32_t u[2][16], v[2][16];
+            take(r, u, v);
+            if (r + step >= blocks) { release(acc); held = false; }
+            if (!slab_of(r, slot)) return;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t sa = lane_at + slot * kMxSlabBytes + (uint32_t)k * 1024u;
+                uint32_t q[4] = {0, 0, 0, 0}, h[4];
+                if (res) ldmatrix_x4_trans(sa, q);
+                rounded(u[k >> 2], v[k >> 2], k & 3, q, h);
+                if (res) __syncwarp();                         // (every lane has read these rows' residuals)
+                stmatrix_x4_trans(sa, h[0], h[1], h[2], h[3]);
+            }
+            hand_over(slot);
         }
         if (held) release(acc);                                // (nothing of this tile is this warp's)
     }
