@@ -188,7 +188,8 @@ typedef struct {
  * npas_quantize_mx and a call on its blob.  path: 0 = automatic, 1 = force the kernel on CUDA cores (fp32; every
  * geometry), 2 = automatic among the tcgen05 kernels, 3 = force the tcgen05 kernel whose 128-row operand are the
  * weights (few rows of X), 4 = force the tcgen05 kernel with persistent tiles, 5 = force the
- * variant of that kernel that runs on CTA pairs (cta_group::2; 4-bit inputs) (NPAS_ERR_UNSUPPORTED when the geometry is outside the requested kernel's envelope). */
+ * variant of that kernel that runs on CTA pairs (cta_group::2; 4-bit inputs), 6 = force the kernel
+ * for up to 16 rows of a 16-bit input (NPAS_ERR_UNSUPPORTED when the geometry is outside the requested kernel's envelope). */
 typedef struct {
     int32_t M, I, O;
     int32_t x_dtype, quantize_x, y_dtype;

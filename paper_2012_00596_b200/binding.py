@@ -444,7 +444,7 @@ def linear_bb_kernel(M: int, blob: BbBlob, *, dtype=torch.bfloat16, out_dtype=No
     return kid.value
 
 
-LINEAR_MX_KERNELS = {1: "linear_mx_simt_kernel", 3: "linear_mx_sw_kernel", 4: "linear_mx_ps_kernel", 5: "linear_mx_d2_kernel"}
+LINEAR_MX_KERNELS = {1: "linear_mx_simt_kernel", 3: "linear_mx_sw_kernel", 4: "linear_mx_ps_kernel", 5: "linear_mx_d2_kernel", 6: "linear_mx_gv_kernel"}
 
 
 def _mx_linear_desc(M, w, dtype, out_dtype, quantize_x, relu, bias, residual, path, variant) -> MxLinearDesc:

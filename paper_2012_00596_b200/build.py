@@ -13,7 +13,7 @@ LIB = os.path.join(HERE, "libnpas.so")
 HOST_SOURCE = os.path.join(CSRC, "host_ext.cpp")
 HOST_LIB = os.path.join(HERE, "_npas_host.so")
 SOURCES = ["api.cu", "host_util.cu", "pack.cu", "conv_simt.cu", "linear_simt.cu", "conv_tc.cu", "conv_kr.cu", "conv_stem.cu", "conv_stem_rows.cu", "conv_dn.cu", "conv_d2.cu", "conv_sk.cu", "linear_tc.cu", "linear_dn.cu", "linear_d2.cu", "linear_sk.cu", "linear_two.cu",
-           "prune.cu", "static_ws.cu", "mx_quant.cu", "linear_mx.cu", "linear_mx_simt.cu", "linear_mx_sw.cu", "linear_mx_ps.cu", "linear_mx_d2.cu"]
+           "prune.cu", "static_ws.cu", "mx_quant.cu", "linear_mx.cu", "linear_mx_simt.cu", "linear_mx_sw.cu", "linear_mx_ps.cu", "linear_mx_d2.cu", "linear_mx_gv.cu"]
 
 
 def _stale() -> bool:

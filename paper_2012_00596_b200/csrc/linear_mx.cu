@@ -20,20 +20,30 @@ npas_status check_args(const npas_mx_linear_desc *d)
     return NPAS_OK;
 }
 
-// 1: CUDA cores, 3: few rows, 4: persistent tiles, 5: the same on CTA pairs.  0: the requested path does not take the geometry.
+// 1: CUDA cores, 3: few rows, 4: persistent tiles, 5: the same on CTA pairs, 6: a 16-bit input of up to 16 rows.  0: the requested path does not take the geometry.
+// Up to 16 rows the kernel for few rows quantises the input itself: every CTA its share, again for every 128 outputs.  (FIXME)
+bool quantizes_itself(const npas_mx_linear_desc &d) { return d.quantize_x && d.M <= 16; }
+
+npas_mx_linear_desc behind_quantize(npas_mx_linear_desc d)
+{
+    if (d.quantize_x) { d.x_dtype = NPAS_MX4; d.quantize_x = 0; }
+    return d;
+}
+
 int kernel_for(const npas_mx_linear_desc &d)
 {
-    npas_mx_linear_desc in = d;
-    if (in.quantize_x) { in.x_dtype = NPAS_MX4; in.quantize_x = 0; }
+    const npas_mx_linear_desc in = behind_quantize(d);
     switch (d.path) {
         case 1: return d.variant ? 0 : 1;
         case 3: return linear_mx_sw_supported(in) ? 3 : 0;
         case 4: return linear_mx_ps_supported(in) ? 4 : 0;
         case 5: return linear_mx_d2_supported(in) ? 5 : 0;
+        case 6: return linear_mx_gv_supported(in) ? 6 : 0;
         case 0: case 2: break;
         default: return 0;
     }
-    if (d.M > 128 && d.O > 128 && linear_mx_d2_supported(in)) return 5;
+    if (linear_mx_gv_supported(in)) return 6;
+    if (d.M > 128 && d.O > 128 && d.I >= 2048 && linear_mx_d2_supported(in)) return 5;
     if (d.M > 128 && linear_mx_ps_supported(in)) return 4;
     if (linear_mx_sw_supported(in)) return 3;
     return d.path == 2 ? 0 : 1;
@@ -46,8 +56,9 @@ int64_t pitch_of(const npas_mx_linear_desc &d) { return ((int64_t)d.I + 7) / 8 *
 // scratch behind the status words: the quantised input, or the copied one
 size_t scratch_bytes(const npas_mx_linear_desc &d)
 {
-    if (d.quantize_x) return mx_layout(d.M, d.I).total;
-    return needs_pitch(d, kernel_for(d)) ? (size_t)d.M * pitch_of(d) * 2 : 0;
+    const int kernel = kernel_for(d);
+    if (d.quantize_x) return kernel == 3 && quantizes_itself(d) ? 0 : mx_layout(d.M, d.I).total;
+    return needs_pitch(d, kernel) ? (size_t)d.M * pitch_of(d) * 2 : 0;
 }
 
 constexpr int kPitchThreads = 256;
@@ -127,13 +138,12 @@ npas_status npas_internal_linear_mx(const npas_mx_linear_desc *d, const void *x,
     if (scratch_size < scratch_bytes(*d)) return NPAS_ERR_BUFFER_TOO_SMALL;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     npas_mx_linear_desc in = *d;
-    if (d->quantize_x) {
+    if (d->quantize_x && !(kernel == 3 && quantizes_itself(*d))) {
         const npas_mx_desc q = {d->M, d->I, NPAS_BF16};
         s = quantize_mx_launch(q, x, scratch, st, Launch());
         if (s != NPAS_OK) return s;
         x = scratch;
-        in.x_dtype = NPAS_MX4;
-        in.quantize_x = 0;
+        in = behind_quantize(in);
     }
     int64_t pitch = d->I;
     if (needs_pitch(*d, kernel)) {
@@ -145,6 +155,7 @@ npas_status npas_internal_linear_mx(const npas_mx_linear_desc *d, const void *x,
     switch (kernel) {
         case 1: return linear_mx_simt_launch(in, x, w, bias, res, y, st);
         case 3: return linear_mx_sw_launch(in, x, pitch, w, bias, res, y, static_cast<uint32_t *>(ws), st);
+        case 6: return linear_mx_gv_launch(in, x, pitch, w, bias, res, y, st);
         case 5: return linear_mx_d2_launch(in, x, w, bias, res, y, static_cast<uint32_t *>(ws), st);
         case 4: return linear_mx_ps_launch(in, x, pitch, w, bias, res, y, static_cast<uint32_t *>(ws), st);
     }

@@ -1,0 +1,130 @@
+// GEMM of a 16-bit input of up to 16 rows with microscaled 4-bit weights: single tokens, where the weights' bytes are the work.
+//
+// Y[m,o] = act(bias[o] + sum_i X[m,i] W[o,i] + residual[m,o]).  With so few rows nothing is read twice, so the weights go from memory
+// to registers, are widened there and multiplied by warp-wide MMAs (m16n8k16, fp32 sums): no stage, barrier or tensor-memory hand-over between
+// the load and the product (linear_mx_sw.cu, whose tensor-core MMAs take the weights from tensor memory, is held up by those: 1x8192 -> 8192
+// 20.7 us, FIXME here).  The order of the columns in an MMA is free as long as both operands agree: a thread takes a whole block of 32
+// columns of a row (16 bytes) and one scale, and of X the same 32 columns (64 bytes) of one row, each exactly as it lies in memory.
+// A block of threads has 32 outputs (8a + g, + 32, + 64, + 96 of a tile of scales, whose 16 bytes hold those four rows), a warp every
+// sixteenth tile of 128 columns of them; the warps' sums meet in shared memory and are added in order.  2.1 instructions a weight,
+// at the issue rate 60 weights a cycle and SM, HBM delivers 46.
+#include "mx_tc.cuh"
+
+namespace npas {
+
+using namespace tc;
+
+namespace {
+
+constexpr int kMaxWarps = 16;
+constexpr int kOutputs = 32;                               // of a block of threads
+
+__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <int NT>
+__global__ void __launch_bounds__(kMaxWarps * 32)
+linear_mx_gv_kernel(int M, int I, int O, int relu, int y_bf16, int nKT, uint32_t pitch, uint64_t off_scales, uint64_t off_values, int64_t x_pitch,
+                    const uint16_t *x, const uint8_t *w, const float *bias, const void *res, void *y)
+{
+    __shared__ float sums[kMaxWarps][kOutputs][NT * 8 + 1];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3, warps = blockDim.x >> 5;
+    const int ot = blockIdx.x >> 2, a8 = (blockIdx.x & 3) * 8;
+    pdl_trigger();
+    pdl_wait();
+    x = behind_wait(x); w = behind_wait(w); bias = behind_wait(bias); res = behind_wait(res);
+    float c[2][NT][4] = {};
+    for (int kt = warp; kt < nKT; kt += warps) {
+        // this thread's block of 32 columns: of four rows of W, and of NT rows of X
+        const int col = kt * kMxTileCols + q * kMxBlock;
+        uint4 e[4], xv[NT][4];
+        const uint4 codes = __ldg(reinterpret_cast<const uint4 *>(w + off_scales + ((uint64_t)ot * nKT + kt) * kMxScaleTile) + a8 + g);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int row = ot * kMxTileRows + 32 * j + a8 + g;
+            e[j] = row < O && col < I ? __ldg(reinterpret_cast<const uint4 *>(w + off_values + (uint64_t)row * pitch + col / 2)) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                xv[t][i] = t * 8 + g < M && col + 8 * i < I ? __ldg(reinterpret_cast<const uint4 *>(x + (int64_t)(t * 8 + g) * x_pitch + col) + i) : make_uint4(0, 0, 0, 0);
+        MxFactor f[4];
+        const uint32_t cw[4] = {codes.x, codes.y, codes.z, codes.w};
+        bool large = false;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t code = cw[j] >> (8 * q) & 255u;
+            f[j] = mx_factor(code);
+            large |= code > 128u;
+        }
+        large = __any_sync(0xFFFFFFFFu, large);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t p[4][4];                                  // of the rows: four pairs of columns
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t word = i == 0 ? e[j].x : i == 1 ? e[j].y : i == 2 ? e[j].z : e[j].w;
+                mx_widen_word(p[j], word, f[j].first);
+            }
+            if (large) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) p[j][k] = mul_bf16x2(p[j][k], f[j].second);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    mma_16816(c[h][t], p[2 * h][0], p[2 * h + 1][0], p[2 * h][1], p[2 * h + 1][1], xv[t][i].x, xv[t][i].y);
+                    mma_16816(c[h][t], p[2 * h][2], p[2 * h + 1][2], p[2 * h][3], p[2 * h + 1][3], xv[t][i].z, xv[t][i].w);
+                }
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sums[warp][(2 * h + (i >> 1)) * 8 + g][t * 8 + 2 * q + (i & 1)] = c[h][t][i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < kOutputs * M; i += blockDim.x) {
+        const int m = i / kOutputs, r = i & (kOutputs - 1), o = ot * kMxTileRows + 32 * (r >> 3) + a8 + (r & 7);
+        if (o >= O) continue;
+        const int64_t at = (int64_t)m * O + o;
+        float v = 0.f;
+        for (int k = 0; k < warps; ++k) v += sums[k][r][m];
+        if (bias) v += __ldg(bias + o);
+        if (res) v += y_bf16 ? bf16_bits_to_f32(__ldg(static_cast<const uint16_t *>(res) + at)) : __ldg(static_cast<const float *>(res) + at);
+        if (relu) v = fmaxf(v, 0.f);
+        if (y_bf16) static_cast<uint16_t *>(y)[at] = (uint16_t)cvt_bf16x2(v, 0.f);
+        else static_cast<float *>(y)[at] = v;
+    }
+}
+
+}  // namespace
+
+bool linear_mx_gv_supported(const npas_mx_linear_desc &d)
+{
+    return d.x_dtype == NPAS_BF16 && !d.quantize_x && d.M <= 16 && !d.variant;
+}
+
+npas_status linear_mx_gv_launch(const npas_mx_linear_desc &d, const void *x, int64_t x_pitch, const void *w, const float *bias, const void *res, void *y,
+                                cudaStream_t st)
+{
+    if (!linear_mx_gv_supported(d)) return NPAS_ERR_UNSUPPORTED;
+    const MxLayout L = mx_layout(d.O, d.I);
+    const int warps = L.nKT < kMaxWarps ? (int)L.nKT : kMaxWarps;
+    const auto kernel = d.M <= 8 ? linear_mx_gv_kernel<1> : linear_mx_gv_kernel<2>;
+    const cudaError_t e = launch_pdl(Launch(), kernel, dim3(L.nRT * 4), dim3((unsigned)(warps * 32)), 0, st, (int)d.M, (int)d.I, (int)d.O, (int)d.relu,
+                                     (int)(d.y_dtype == NPAS_BF16), (int)L.nKT, L.pitch, L.off_scales, L.off_values, x_pitch, static_cast<const uint16_t *>(x),
+                                     static_cast<const uint8_t *>(w), bias, res, y);
+    count_launch();
+    return e == cudaSuccess ? launch_status() : NPAS_ERR_CUDA;
+}
+
+}  // namespace npas

@@ -7,6 +7,8 @@
 // results do not depend on timing.  Tensor memory lane = output, column = input row: the epilogue's stores are 32 consecutive outputs a warp.
 //   4-bit input: both operands by TMA as they lie in the blobs, scales copied from shared into tensor memory ahead of the MMAs of a
 //     step (a set of columns per ring stage, so that no copy meets an MMA that still reads), MMAs of kind::mxf4 over 64 columns.
+//   16-bit input to be quantised: the eight warps that have nothing to do before the epilogue quantise the CTA's share of X into the stage, a row
+//     of 256 columns a warp, instead of a launch of its own ahead of this one (a call of one row 6.0 -> FIXME us of host time).
 //   16-bit input: eight warps widen the weights, a thread a row: 32 bytes -> 64 bf16 values in 32 columns of tensor memory, from where the
 //     MMAs of kind::f16 take their first operand.  Four such slots; weights and inputs have rings of their own (256 and 64 columns a
 //     stage).  Widening costs 2.4 instructions a weight, at the issue rate about what HBM delivers.
@@ -27,14 +29,14 @@ constexpr int kRows = 128;
 constexpr int kStepCols = 256;                             // columns of a weight stage
 constexpr int kMaxStages = 6, kMaxXStages = 8, kSlots = 4;
 constexpr int kMaxSplit = 8;                               // portable cluster size
-constexpr uint32_t kSmemLimit = 232448;
+constexpr uint32_t kSmemLimit = 232448, kSmemHalf = 115712;   // of a CTA alone on its SM, of one of two (1 KB each is the system's)
 constexpr uint32_t kWBytes = kRows * 128;
 constexpr uint32_t kScaleBytes = 2 * kMxScaleTile;         // of 128 rows and a stage
 
 struct MxSwParams {
     int M, I, O, N, KS, nS, spr, nMT, nOT, nKT, S, SX, cpr;   // spr: steps per CTA; SX: stages of the input (16 bits); cpr: input rows a CTA owns
     int relu, y_bf16;
-    uint32_t x_bytes, stage_bytes, off_x, off_red, off_bar, smem_bytes, tmem_cols, tmem_scales;
+    uint32_t x_bytes, stage_bytes, off_x, off_red, red_pitch, off_bar, smem_bytes, tmem_cols, tmem_scales;
     uint64_t w_scales, x_scales;                           // offsets of the scales in the blobs
 };
 
@@ -50,6 +52,10 @@ struct MxSwBars {
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
+__device__ __forceinline__ void st_cluster_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
 __device__ __forceinline__ float load_res(const void *res, int64_t at, int y_bf16)
 {
     return y_bf16 ? bf16_bits_to_f32(__ldg(static_cast<const uint16_t *>(res) + at)) : __ldg(static_cast<const float *>(res) + at);
@@ -61,11 +67,15 @@ __device__ __forceinline__ void store_y(void *y, int64_t at, float v, int relu, 
     else static_cast<float *>(y)[at] = v;
 }
 
-template <bool kMx>
-__global__ void __launch_bounds__(kThreads, 1)
-linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w, const MxSwParams p, const uint8_t *xblob,
+// what the input is: a blob, 16 bits to be quantised, 16 bits
+enum MxIn { kBlob, kQuantize, kWide };
+
+template <MxIn kIn>
+__global__ void __launch_bounds__(kThreads, 2)
+linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w, const MxSwParams p, const uint8_t *xin,
                     const uint8_t *wblob, const float *bias, const void *res, void *y, uint32_t *ws)
 {
+    constexpr bool kMx = kIn != kWide;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     MxSwBars *bars = reinterpret_cast<MxSwBars *>(smem + p.off_bar);
@@ -80,13 +90,13 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
     const int k_n = max(0, min((p.I + 63) / 64 - s_lo * 4, s_n * 4));
 
     if (tid == 0) {
-        for (int s = 0; s < p.S; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], kMx ? 1 : kEpiWarps); }
+        for (int s = 0; s < p.S; ++s) { mbar_init(&bars->full[s], kIn == kQuantize ? 1 + kEpiWarps : 1); mbar_init(&bars->empty[s], kMx ? 1 : kEpiWarps); }
         for (int s = 0; s < p.SX; ++s) { mbar_init(&bars->x_full[s], 1); mbar_init(&bars->x_empty[s], 1); }
         for (int s = 0; s < kSlots; ++s) { mbar_init(&bars->slot_full[s], kEpiWarps / 2); mbar_init(&bars->slot_empty[s], 1); }
         mbar_init(&bars->acc_full, 1);
         bars->abort_flag = 0;
         fence_barrier_init();
-        prefetch_tensormap(&tmap_x);
+        if (kIn != kQuantize) prefetch_tensormap(&tmap_x);
         prefetch_tensormap(&tmap_w);
     }
     if (warp == 1) tmem_alloc(&bars->tmem_base, p.tmem_cols);
@@ -98,6 +108,7 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
     if (p.KS > 1) cluster_arrive();    // this CTA is running: its shared memory may be written by the others
     pdl_wait();
     const int z = zero_behind_wait();
+    xin = behind_wait(xin); wblob = behind_wait(wblob);
 
     // bytes of scales of stage `step`: the last tile of columns may stand alone
     auto scale_bytes = [&](int step) { return (uint32_t)min(2, p.nKT - 2 * step) * kMxScaleTile; };
@@ -110,12 +121,12 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
                 uint8_t *st = smem + (size_t)s * p.stage_bytes;
                 const int step = s_lo + i;
                 const uint32_t sb = scale_bytes(step);
-                mbar_arrive_expect_tx(&bars->full[s], kWBytes + sb + (kMx ? p.x_bytes + sb : 0u));
+                mbar_arrive_expect_tx(&bars->full[s], kWBytes + sb + (kIn == kBlob ? p.x_bytes + sb : 0u));
                 tma_load_2d(st, &tmap_w, &bars->full[s], step * 128, ot * kRows);
                 bulk_load_1d(st + kWBytes, wblob + p.w_scales + ((uint64_t)ot * p.nKT + 2 * step) * kMxScaleTile, sb, &bars->full[s]);
-                if (kMx) {
+                if (kIn == kBlob) {
                     tma_load_2d(st + kWBytes + 2 * kScaleBytes, &tmap_x, &bars->full[s], step * 128, mt * kRows);
-                    bulk_load_1d(st + kWBytes + kScaleBytes, xblob + p.x_scales + ((uint64_t)mt * p.nKT + 2 * step) * kMxScaleTile, sb, &bars->full[s]);
+                    bulk_load_1d(st + kWBytes + kScaleBytes, xin + p.x_scales + ((uint64_t)mt * p.nKT + 2 * step) * kMxScaleTile, sb, &bars->full[s]);
                 }
                 if (++s == (uint32_t)p.S) { s = 0; ++lap; }
             }
@@ -175,7 +186,36 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
             }
         }
         __syncwarp();
-    } else if (!kMx) {
+    } else if (kIn == kQuantize) {
+        // ---- quantising: a warp takes 256 columns of a row, eight a lane, and writes them as the TMA would (16-byte pieces XOR-ed with the
+        // row number) and their scales as they lie in a blob; rows past the last are left as they are (their sums are nobody's) -----------
+        const uint16_t *x = reinterpret_cast<const uint16_t *>(xin);
+        const int rows = min(p.N, p.M - mt * p.N);
+        const bool whole = p.I % 8 == 0;
+        uint32_t s = 0, lap = 0;
+        for (int i = 0; i < s_n; ++i) {
+            if (lap >= 1 && !__all_sync(0xFFFFFFFFu, mbar_wait(&bars->empty[s], (lap & 1u) ^ 1u, abort_flag, ws, 0xA120))) break;
+            uint8_t *st = smem + (size_t)s * p.stage_bytes;
+            const int c = (s_lo + i) * kStepCols + lane * 8;
+            for (int r = warp - 2; r < rows; r += kEpiWarps) {
+                uint32_t v[4];
+                mx_load8(v, x + (int64_t)(mt * p.N + r) * p.I, c, p.I, whole);
+                uint32_t top = mx_top8(v);
+                top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+                top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+                const uint32_t code = mx_code(top);
+                float f[8];
+                mx_scaled8(f, v, code);
+                const uint32_t word = mx_cvt_e2m1x8(f);
+                *reinterpret_cast<uint32_t *>(st + kWBytes + 2 * kScaleBytes + r * 128 + (((lane >> 2) ^ (r & 7)) * 16) + (lane & 3) * 4) = code == 255 ? 0u : word;
+                if ((lane & 3) == 0) st[kWBytes + kScaleBytes + (lane >> 4) * kMxScaleTile + mx_scale_at((uint32_t)r, (uint32_t)lane >> 2)] = (uint8_t)code;
+            }
+            fence_proxy_async_smem();                          // the tensor core reads what this thread wrote
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars->full[s]);
+            if (++s == (uint32_t)p.S) { s = 0; ++lap; }
+        }
+    } else if (kIn == kWide) {
         // ---- widening: group g of four warps takes every second K step, a thread one row of the weights -----------------
         const int group = (warp - 2) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
         bool ok = true;
@@ -229,13 +269,14 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
                     for (int i = 0; i < 16; ++i)
                         if (o < p.O && c0 + i < rows) store_y(y, (int64_t)(mt * p.N + c0 + i) * p.O + o, __uint_as_float(v[i]) + b + add[i], p.relu, p.y_bf16);
                 } else {
+                    // four rows of X at a time to the CTA that owns them: [rank][output][its rows] floats, an output's padded by 16 bytes
                     tmem_ld_wait();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
+                    for (int i = 0; i < 16; i += 4) {
                         const int m = c0 + i, owner = m / p.cpr;
                         if (m < rows)
-                            st_remote_u32(map_to_cta(smem_u32(smem + p.off_red), (uint32_t)owner) +
-                                              (uint32_t)((rank * p.cpr + m - owner * p.cpr) * kRows + quarter * 32 + lane) * 4u, v[i]);
+                            st_cluster_v4(map_to_cta(smem_u32(smem + p.off_red), (uint32_t)owner) + (uint32_t)(rank * kRows + quarter * 32 + lane) * p.red_pitch +
+                                              (uint32_t)(m - owner * p.cpr) * 4u, v[i], v[i + 1], v[i + 2], v[i + 3]);
                     }
                 }
             }
@@ -254,21 +295,28 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
     }
     if (p.KS == 1) return;
     const int own = max(0, min(p.cpr, rows - rank * p.cpr));
-    for (int i = tid; i < own * kRows; i += kThreads) {
-        const int m = i / kRows, ol = i - m * kRows, o = ot * kRows + ol;
+    for (int i = tid; i < (own + 3) / 4 * kRows; i += kThreads) {
+        const int m0 = i / kRows * 4, ol = i & (kRows - 1), o = ot * kRows + ol;
         if (o >= p.O) continue;
-        const int64_t at = (int64_t)(mt * p.N + rank * p.cpr + m) * p.O + o + z;
-        const float add = res ? load_res(res, at, p.y_bf16) : 0.f;
-        float v = 0.f;
-        for (int s = 0; s < live; ++s) v += *reinterpret_cast<const float *>(smem + p.off_red + (uint32_t)((s * p.cpr + m) * kRows + ol) * 4u);
-        if (bias) v += __ldg(bias + o + z);
-        store_y(y, at, v + add, p.relu, p.y_bf16);
+        const int64_t at = (int64_t)(mt * p.N + rank * p.cpr + m0) * p.O + o + z;
+        float add[4], v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) add[j] = res && m0 + j < own ? load_res(res, at + (int64_t)j * p.O, p.y_bf16) : 0.f;
+        const uint8_t *src = smem + p.off_red + (uint32_t)ol * p.red_pitch + (uint32_t)m0 * 4u;
+        for (int s = 0; s < live; ++s, src += kRows * p.red_pitch) {
+            const float4 u = *reinterpret_cast<const float4 *>(src);
+            v[0] += u.x; v[1] += u.y; v[2] += u.z; v[3] += u.w;
+        }
+        const float b = bias ? __ldg(bias + o + z) : 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (m0 + j < own) store_y(y, at + (int64_t)j * p.O, v[j] + b + add[j], p.relu, p.y_bf16);
     }
 }
 
 bool plan(const npas_mx_linear_desc &d, MxSwParams &p, int sms)
 {
-    const bool mx = d.x_dtype == NPAS_MX4;
+    const bool mx = d.x_dtype == NPAS_MX4 || d.quantize_x;
     const MxLayout LW = mx_layout(d.O, d.I), LX = mx_layout(d.M, d.I);
     p = MxSwParams{};
     p.M = d.M; p.I = d.I; p.O = d.O;
@@ -280,29 +328,35 @@ bool plan(const npas_mx_linear_desc &d, MxSwParams &p, int sms)
     // Input rows of a tile: all of them, or equal shares in multiples of 16 (4-bit: a tile starts where a tile of scales does)
     p.N = mx && p.nMT > 1 ? kRows : ((d.M + p.nMT - 1) / p.nMT + 15) / 16 * 16;
     p.w_scales = LW.off_scales; p.x_scales = LX.off_scales;
-    // Split of the columns: as many CTAs as one wave holds
+    // Split of the columns: up to a CTA per SM, two where weights are widened (which takes longer than they take to arrive); eight only while
+    // the clusters fill less than half the chip (more do not fit side by side: 32x2048 -> 2048 4.8 us in fours, 5.5 in eights)
     const long long tiles = (long long)p.nMT * p.nOT;
     if (tiles > 0x7FFFFFFF / kMaxSplit) return false;
     p.KS = 1;
-    while (p.KS < kMaxSplit && 2 * p.KS <= p.nS && tiles * 2 * p.KS <= sms) p.KS *= 2;
+    while (p.KS < kMaxSplit && 2 * p.KS <= p.nS && tiles * 2 * p.KS <= (2 * p.KS == 8 ? sms / 2 : mx ? sms : 2 * sms)) p.KS *= 2;
     if (d.variant) {
         p.KS = d.variant;
         if (p.KS < 1 || p.KS > kMaxSplit || p.KS & (p.KS - 1)) return false;
     }
     p.spr = (p.nS + p.KS - 1) / p.KS;
-    p.cpr = (p.N + p.KS - 1) / p.KS;
-    const uint32_t red = p.KS > 1 ? (uint32_t)p.KS * p.cpr * kRows * 4u : 0u;
+    p.cpr = ((p.N + p.KS - 1) / p.KS + 3) / 4 * 4;
+    p.red_pitch = (uint32_t)p.cpr * 4u + 16u;
+    const uint32_t red = p.KS > 1 ? (uint32_t)p.KS * kRows * p.red_pitch : 0u;
     const uint32_t fixed = red + (uint32_t)sizeof(MxSwBars) + 128u + 1024u;
     p.x_bytes = (uint32_t)p.N * 128u;
     p.stage_bytes = round_up(kWBytes + (mx ? 2 * kScaleBytes + p.x_bytes : kScaleBytes), 1024);
-    const uint32_t budget = kSmemLimit - fixed;
+    // (two CTAs on an SM where there are more CTAs than SMs)
+    const uint32_t limit = tiles * p.KS > sms ? kSmemHalf : kSmemLimit;
+    if (fixed >= limit) return false;
+    const uint32_t budget = limit - fixed;
     if (mx) {
         p.S = (int)(budget / p.stage_bytes);
         p.SX = 0;
     } else {
         // the input's ring (of 64 columns a stage)
         p.SX = kMaxXStages;
-        while (p.SX > 3 && (uint32_t)p.SX * p.x_bytes + 3 * p.stage_bytes > budget) --p.SX;
+        while (p.SX > 2 && (uint32_t)p.SX * p.x_bytes + 3 * p.stage_bytes > budget) --p.SX;
+        if ((uint32_t)p.SX * p.x_bytes >= budget) return false;
         p.S = (int)((budget - (uint32_t)p.SX * p.x_bytes) / p.stage_bytes);
     }
     if (p.S > kMaxStages) p.S = kMaxStages;
@@ -340,13 +394,14 @@ npas_status linear_mx_sw_launch(const npas_mx_linear_desc &d, const void *x, int
 {
     MxSwParams p;
     if (!planned(d, p)) return NPAS_ERR_UNSUPPORTED;
-    const bool mx = d.x_dtype == NPAS_MX4;
+    const bool blob = d.x_dtype == NPAS_MX4;
     CUtensorMap tmx, tmw;
     if (!mx_encode_values(&tmw, w, mx_layout(d.O, d.I), d.O, kRows)) return NPAS_ERR_CUDA;
-    if (!(mx ? mx_encode_values(&tmx, x, mx_layout(d.M, d.I), d.M, (uint32_t)p.N)
-             : mx_encode_bf16(&tmx, x, (uint64_t)d.I, (uint64_t)x_pitch, (uint64_t)d.M, (uint32_t)p.N)))
+    if (d.quantize_x) tmx = tmw;
+    else if (!(blob ? mx_encode_values(&tmx, x, mx_layout(d.M, d.I), d.M, (uint32_t)p.N)
+                    : mx_encode_bf16(&tmx, x, (uint64_t)d.I, (uint64_t)x_pitch, (uint64_t)d.M, (uint32_t)p.N)))
         return NPAS_ERR_CUDA;
-    const auto kernel = mx ? linear_mx_sw_kernel<true> : linear_mx_sw_kernel<false>;
+    const auto kernel = blob ? linear_mx_sw_kernel<kBlob> : d.quantize_x ? linear_mx_sw_kernel<kQuantize> : linear_mx_sw_kernel<kWide>;
     if (allow_dynamic_smem(reinterpret_cast<const void *>(kernel), (int)kSmemLimit) != NPAS_OK) return NPAS_ERR_CUDA;
     const dim3 grid((unsigned)(p.nMT * p.nOT * p.KS)), block(kThreads);
     const uint8_t *xb = static_cast<const uint8_t *>(x), *wb = static_cast<const uint8_t *>(w);

@@ -80,6 +80,9 @@ npas_status linear_mx_ps_launch(const npas_mx_linear_desc &d, const void *x, int
 bool linear_mx_d2_supported(const npas_mx_linear_desc &d);
 npas_status linear_mx_d2_launch(const npas_mx_linear_desc &d, const void *x, const void *w, const float *bias, const void *res, void *y, uint32_t *ws,
                                 cudaStream_t st);
+bool linear_mx_gv_supported(const npas_mx_linear_desc &d);
+npas_status linear_mx_gv_launch(const npas_mx_linear_desc &d, const void *x, int64_t x_pitch, const void *w, const float *bias, const void *res, void *y,
+                                cudaStream_t st);
 npas_status linear_mx_simt_launch(const npas_mx_linear_desc &d, const void *x, const void *w, const float *bias, const void *res, void *y,
                                   cudaStream_t st);
 

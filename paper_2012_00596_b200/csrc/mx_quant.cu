@@ -19,81 +19,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Eight floats -> a word of e2m1 elements in the order of mx_nibble: to nearest even, past 6 to 6.
-__device__ __forceinline__ uint32_t cvt_e2m1x8(const float (&v)[8])
-{
-    uint32_t d;
-    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 a, %3, %1;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 b, %7, %5;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 c, %4, %2;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %6;\n\t"
-        "mov.b32 %0, {a, b, c, d};\n\t}"
-        : "=r"(d) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
-    return d;
-}
-
-// Eight columns of a row as they are, zeros past the end (bf16 in pairs: four words; fp32: eight).  `whole`: rows start on 16-byte
-// boundaries and 8 divides the columns.
-template <int W>
-__device__ __forceinline__ void load8(uint32_t (&v)[W], const void *row, int c, int cols, bool whole)
-{
-    constexpr bool kHalf = W == 4;
-#pragma unroll
-    for (int i = 0; i < W; ++i) v[i] = 0u;
-    if (whole) {
-        if (c >= cols) return;
-        if constexpr (kHalf) {
-            const uint4 u = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(row) + c);
-            v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
-        } else {
-            tc::ld_sector(v, static_cast<const uint32_t *>(row) + c);
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (c + i < cols) {
-            if constexpr (kHalf) v[i / 2] |= (uint32_t)static_cast<const uint16_t *>(row)[c + i] << (16 * (i & 1));
-            else v[i] = static_cast<const uint32_t *>(row)[c + i];
-        }
-}
-
-// largest magnitude of the eight, the upper half of its bits (infinities and NaN come out above every number)
-template <int W>
-__device__ __forceinline__ uint32_t top8(const uint32_t (&v)[W])
-{
-    if constexpr (W == 4) {
-        uint32_t m = __vmaxu2(__vmaxu2(v[0] & 0x7FFF7FFFu, v[1] & 0x7FFF7FFFu), __vmaxu2(v[2] & 0x7FFF7FFFu, v[3] & 0x7FFF7FFFu));
-        return max(m & 0xFFFFu, m >> 16);
-    } else {
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, v[i] & 0x7FFFFFFFu);
-        return m >> 16;
-    }
-}
-
-// the eight times 2^(127 - code), as floats.  (In pairs of bf16 where they are: what falls below bf16's smallest number is far below 1/4.)
-template <int W>
-__device__ __forceinline__ void scaled8(float (&f)[8], const uint32_t (&v)[W], uint32_t code)
-{
-    const uint32_t e = 254u - min(code, 253u);                 // (the NaN block's elements mean nothing)
-    if constexpr (W == 4) {
-        const uint32_t inv = e * 0x00800080u;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t u = tc::mul_bf16x2(v[i], inv);
-            f[2 * i] = __uint_as_float(u << 16);
-            f[2 * i + 1] = __uint_as_float(u & 0xFFFF0000u);
-        }
-    } else {
-        const float inv = __uint_as_float(e << 23);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[i]) * inv;
-    }
-}
-
 template <typename T, bool kParts, int kLanes>
 __global__ void __launch_bounds__(kThreads) quantize_mx_kernel(int rows, int cols, int whole, int n_parts, const T *src, uint8_t *blob)
 {
@@ -123,7 +48,7 @@ __global__ void __launch_bounds__(kThreads) quantize_mx_kernel(int rows, int col
 #pragma unroll
     for (int p = 0; p < kPasses; ++p) {
         if (p >= passes) break;
-        load8(v[p], from, p * kRowsPerPass < left ? c : cols, cols, whole);
+        tc::mx_load8(v[p], from, p * kRowsPerPass < left ? c : cols, cols, whole);
         from += (int64_t)kRowsPerPass * cols;
     }
     uint8_t *to = values + (uint64_t)row0 * L.pitch + c / 2;
@@ -132,13 +57,13 @@ __global__ void __launch_bounds__(kThreads) quantize_mx_kernel(int rows, int col
     for (int p = 0; p < kPasses; ++p) {
         if (p >= passes) break;
         const int r = p * kRowsPerPass + r0;
-        uint32_t top = top8(v[p]);
+        uint32_t top = tc::mx_top8(v[p]);
         top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
         top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-        const uint32_t e = top >> 7, code = e == 255 ? 255u : e > 2 ? e - 2 : 0u;
+        const uint32_t code = tc::mx_code(top);
         float f[8];
-        scaled8(f, v[p], code);
-        const uint32_t word = cvt_e2m1x8(f);
+        tc::mx_scaled8(f, v[p], code);
+        const uint32_t word = tc::mx_cvt_e2m1x8(f);
         if (p * kRowsPerPass < left && stored) *reinterpret_cast<uint32_t *>(to) = code == 255 ? 0u : word;
         to += (uint64_t)kRowsPerPass * L.pitch;
         if ((lane & 3) == 0) scales[mx_scale_at((uint32_t)r, (uint32_t)lane >> 2)] = (uint8_t)code;   // (rows and blocks past the end: 0)

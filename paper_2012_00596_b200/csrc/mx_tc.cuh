@@ -114,13 +114,17 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
     return d;
 }
 
-// Pair i (columns 2i, 2i + 1) of a word of eight elements as bf16 times 2^-126: the magnitude bits are exponent and mantissa.
-template <int i>
-__device__ __forceinline__ uint32_t mx_pair_small(uint32_t w)
+// A word of eight elements -> four pairs of bf16 values (columns 2i, 2i + 1), times `factor` (mx_factor).  A pair's two nibbles lie 16 bits
+// apart: times 2^12 + 2^6 their signs and, once more, their magnitudes come to where a bf16 number has its sign and the last two exponent
+// bits and first mantissa bit (elements 2^-126 times their size, subnormals included).  The multiplications take the place of shifts, of
+// which an SM does half as many a cycle.
+__device__ __forceinline__ void mx_widen_word(uint32_t (&p)[4], uint32_t w, uint32_t factor)
 {
-    constexpr int up = 6 - 4 * i;
-    const uint32_t mag = up >= 0 ? w << (up >= 0 ? up : 0) : w >> (up < 0 ? -up : 0);
-    return (mag & 0x01C001C0u) | ((w << (12 - 4 * i)) & 0x80008000u);
+    const uint32_t v = w >> 8;
+    p[0] = mul_bf16x2(((w & 0x000F000Fu) * 0x1040u) & 0x81C081C0u, factor);
+    p[1] = mul_bf16x2(((w & 0x00F000F0u) * 0x0104u) & 0x81C081C0u, factor);
+    p[2] = mul_bf16x2(((v & 0x000F000Fu) * 0x1040u) & 0x81C081C0u, factor);
+    p[3] = mul_bf16x2(((v & 0x00F000F0u) * 0x0104u) & 0x81C081C0u, factor);
 }
 
 // What a block's elements, 2^-126 times their size, are multiplied by to become bf16 values: 2^126 times the scale, in two factors
@@ -141,16 +145,97 @@ __device__ __forceinline__ void mx_widen(uint32_t (&r)[32], const uint4 &a, cons
     const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const uint32_t f = j < 4 ? f0.first : f1.first;
-        r[4 * j] = mul_bf16x2(mx_pair_small<0>(w[j]), f);
-        r[4 * j + 1] = mul_bf16x2(mx_pair_small<1>(w[j]), f);
-        r[4 * j + 2] = mul_bf16x2(mx_pair_small<2>(w[j]), f);
-        r[4 * j + 3] = mul_bf16x2(mx_pair_small<3>(w[j]), f);
+        uint32_t p[4];
+        mx_widen_word(p, w[j], j < 4 ? f0.first : f1.first);
+        r[4 * j] = p[0]; r[4 * j + 1] = p[1]; r[4 * j + 2] = p[2]; r[4 * j + 3] = p[3];
     }
     if (__any_sync(0xFFFFFFFFu, code0 > 128u || code1 > 128u)) {
 #pragma unroll
         for (int j = 0; j < 32; ++j) r[j] = mul_bf16x2(r[j], j < 16 ? f0.second : f1.second);
     }
+}
+
+// ---- quantising: eight columns of a row ----------------------------------------------------------------
+// Eight floats -> a word of e2m1 elements in the order of mx_nibble: to nearest even, past 6 to 6.
+__device__ __forceinline__ uint32_t mx_cvt_e2m1x8(const float (&v)[8])
+{
+    uint32_t d;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %3, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %7, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %4, %2;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %6;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(d) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return d;
+}
+
+// Eight columns of a row as they are, zeros past the end (bf16 in pairs: four words; fp32: eight).  `whole`: rows start on 16-byte
+// boundaries and 8 divides the columns.
+template <int W>
+__device__ __forceinline__ void mx_load8(uint32_t (&v)[W], const void *row, int c, int cols, bool whole)
+{
+    constexpr bool kHalf = W == 4;
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = 0u;
+    if (whole) {
+        if (c >= cols) return;
+        if constexpr (kHalf) {
+            const uint4 u = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(row) + c);
+            v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
+        } else {
+            ld_sector(v, static_cast<const uint32_t *>(row) + c);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c + i < cols) {
+            if constexpr (kHalf) v[i / 2] |= (uint32_t)static_cast<const uint16_t *>(row)[c + i] << (16 * (i & 1));
+            else v[i] = static_cast<const uint32_t *>(row)[c + i];
+        }
+}
+
+// largest magnitude of the eight, the upper half of its bits (infinities and NaN come out above every number)
+template <int W>
+__device__ __forceinline__ uint32_t mx_top8(const uint32_t (&v)[W])
+{
+    if constexpr (W == 4) {
+        uint32_t m = __vmaxu2(__vmaxu2(v[0] & 0x7FFF7FFFu, v[1] & 0x7FFF7FFFu), __vmaxu2(v[2] & 0x7FFF7FFFu, v[3] & 0x7FFF7FFFu));
+        return max(m & 0xFFFFu, m >> 16);
+    } else {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, v[i] & 0x7FFFFFFFu);
+        return m >> 16;
+    }
+}
+
+// the eight times 2^(127 - code), as floats.  (In pairs of bf16 where they are: what falls below bf16's smallest number is far below 1/4.)
+template <int W>
+__device__ __forceinline__ void mx_scaled8(float (&f)[8], const uint32_t (&v)[W], uint32_t code)
+{
+    const uint32_t e = 254u - min(code, 253u);                 // (the NaN block's elements mean nothing)
+    if constexpr (W == 4) {
+        const uint32_t inv = e * 0x00800080u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t u = mul_bf16x2(v[i], inv);
+            f[2 * i] = __uint_as_float(u << 16);
+            f[2 * i + 1] = __uint_as_float(u & 0xFFFF0000u);
+        }
+    } else {
+        const float inv = __uint_as_float(e << 23);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[i]) * inv;
+    }
+}
+
+// The scale code of a block from the upper half of its largest magnitude: its exponent less two, 255 for infinities and NaN.
+__device__ __forceinline__ uint32_t mx_code(uint32_t top)
+{
+    const uint32_t e = top >> 7;
+    return e == 255 ? 255u : e > 2 ? e - 2 : 0u;
 }
 
 // ---- host: tensor maps ------------------------------------------------------------------------

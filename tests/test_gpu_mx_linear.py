@@ -260,7 +260,7 @@ def test_refusals():
         with pytest.raises(AssertionError):
             npas.linear_mx(kw.pop("x"), w, kw.pop("bias"), kw.pop("residual"), **kw)
     for bad, code in ((dict(x=x.float()), 3), (dict(x=c["x"].cuda()[:, :32].contiguous()), 2), (dict(x=x[:0]), 2), (dict(path=77), 8),
-                      (dict(ws=npas.workspace(), quantize_x=True), 7), (dict(x=npas.quantize_mx(x), quantize_x=True), 3), (dict(out=x.view(-1)[:128].view(4, 32)), 8)):
+                      (dict(x=torch.zeros(400, 64, dtype=torch.bfloat16, device="cuda"), ws=npas.workspace(), quantize_x=True), 7), (dict(x=npas.quantize_mx(x), quantize_x=True), 3), (dict(out=x.view(-1)[:128].view(4, 32)), 8)):
         kw = dict(x=x)
         kw.update(bad)
         with pytest.raises(npas.NpasError) as e:
