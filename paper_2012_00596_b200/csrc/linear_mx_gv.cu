@@ -25,6 +25,14 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// A thread's share of a tile of 128 columns: a block of 32 of four rows of W and their scales; and the same columns of NT rows of X.
+struct Share {
+    uint4 e[4], codes;
+};
+template <int NT> struct ShareX {
+    uint4 x[NT][4];
+};
+
 template <int NT>
 __global__ void __launch_bounds__(kMaxWarps * 32)
 linear_mx_gv_kernel(int M, int I, int O, int relu, int y_bf16, int nKT, uint32_t pitch, uint64_t off_scales, uint64_t off_values, int64_t x_pitch,
@@ -37,53 +45,74 @@ linear_mx_gv_kernel(int M, int I, int O, int relu, int y_bf16, int nKT, uint32_t
     pdl_wait();
     x = behind_wait(x); w = behind_wait(w); bias = behind_wait(bias); res = behind_wait(res);
     float c[2][NT][4] = {};
-    for (int kt = warp; kt < nKT; kt += warps) {
-        // this thread's block of 32 columns: of four rows of W, and of NT rows of X
-        const int col = kt * kMxTileCols + q * kMxBlock;
-        uint4 e[4], xv[NT][4];
-        const uint4 codes = __ldg(reinterpret_cast<const uint4 *>(w + off_scales + ((uint64_t)ot * nKT + kt) * kMxScaleTile) + a8 + g);
+    const int row0 = ot * kMxTileRows + a8 + g;
+    const uint8_t *e0 = w + off_values + (uint64_t)row0 * pitch + q * (kMxBlock / 2);
+    const uint4 *s0 = reinterpret_cast<const uint4 *>(w + off_scales + (uint64_t)ot * nKT * kMxScaleTile) + a8 + g;
+    const uint16_t *x0 = x + (int64_t)g * x_pitch + q * kMxBlock;
+    auto load = [&](Share &v, int kt) {
+        const int left = I - (kt * kMxTileCols + q * kMxBlock);            // columns there are from this thread's first one on
+        v.codes = __ldg(s0 + (int64_t)kt * (kMxScaleTile / 16));
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int row = ot * kMxTileRows + 32 * j + a8 + g;
-            e[j] = row < O && col < I ? __ldg(reinterpret_cast<const uint4 *>(w + off_values + (uint64_t)row * pitch + col / 2)) : make_uint4(0, 0, 0, 0);
-        }
+        for (int j = 0; j < 4; ++j)
+            v.e[j] = row0 + 32 * j < O && left > 0 ? __ldg(reinterpret_cast<const uint4 *>(e0 + (uint64_t)(32 * j) * pitch + (uint32_t)kt * (kMxTileCols / 2)))
+                                                   : make_uint4(0, 0, 0, 0);
+    };
+    auto load_x = [&](ShareX<NT> &v, int kt) {
+        const int left = I - (kt * kMxTileCols + q * kMxBlock);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                xv[t][i] = t * 8 + g < M && col + 8 * i < I ? __ldg(reinterpret_cast<const uint4 *>(x + (int64_t)(t * 8 + g) * x_pitch + col) + i) : make_uint4(0, 0, 0, 0);
-        MxFactor f[4];
-        const uint32_t cw[4] = {codes.x, codes.y, codes.z, codes.w};
-        bool large = false;
+                v.x[t][i] = t * 8 + g < M && 8 * i < left ? __ldg(reinterpret_cast<const uint4 *>(x0 + (int64_t)t * 8 * x_pitch + kt * kMxTileCols) + i)
+                                                          : make_uint4(0, 0, 0, 0);
+    };
+    auto multiply = [&](const Share &v, const ShareX<NT> &vx) {
+        uint32_t code[4], f[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t code = cw[j] >> (8 * q) & 255u;
-            f[j] = mx_factor(code);
-            large |= code > 128u;
+            code[j] = (j == 0 ? v.codes.x : j == 1 ? v.codes.y : j == 2 ? v.codes.z : v.codes.w) >> (8 * q) & 255u;
+            f[j] = mx_factor(code[j]).first;
         }
-        large = __any_sync(0xFFFFFFFFu, large);
+        const bool large = __any_sync(0xFFFFFFFFu, max(max(code[0], code[1]), max(code[2], code[3])) > 128u);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             uint32_t p[4][4];                                  // of the rows: four pairs of columns
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t word = i == 0 ? e[j].x : i == 1 ? e[j].y : i == 2 ? e[j].z : e[j].w;
-                mx_widen_word(p[j], word, f[j].first);
+                const uint32_t word = i == 0 ? v.e[j].x : i == 1 ? v.e[j].y : i == 2 ? v.e[j].z : v.e[j].w;
+                mx_widen_word(p[j], word, f[j]);
             }
             if (large) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) p[j][k] = mul_bf16x2(p[j][k], f[j].second);
+                    for (int k = 0; k < 4; ++k) p[j][k] = mul_bf16x2(p[j][k], mx_factor(code[j]).second);
             }
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    mma_16816(c[h][t], p[2 * h][0], p[2 * h + 1][0], p[2 * h][1], p[2 * h + 1][1], xv[t][i].x, xv[t][i].y);
-                    mma_16816(c[h][t], p[2 * h][2], p[2 * h + 1][2], p[2 * h][3], p[2 * h + 1][3], xv[t][i].z, xv[t][i].w);
+                    mma_16816(c[h][t], p[2 * h][0], p[2 * h + 1][0], p[2 * h][1], p[2 * h + 1][1], vx.x[t][i].x, vx.x[t][i].y);
+                    mma_16816(c[h][t], p[2 * h][2], p[2 * h + 1][2], p[2 * h][3], p[2 * h + 1][3], vx.x[t][i].z, vx.x[t][i].w);
                 }
         }
+    };
+    // the next share is on its way while one is multiplied (of X only where the registers are there for it: it comes from L2)
+    constexpr bool kAheadX = NT == 1;
+    Share a, b;
+    ShareX<NT> ax, bx;
+    int kt = warp;
+    if (kt < nKT) { load(a, kt); if (kAheadX) load_x(ax, kt); }
+    while (kt < nKT) {
+        const int next = kt + warps, third = next + warps;
+        if (!kAheadX) load_x(ax, kt);
+        if (next < nKT) { load(b, next); if (kAheadX) load_x(bx, next); }
+        multiply(a, ax);
+        if (next >= nKT) break;
+        if (!kAheadX) load_x(bx, next);
+        if (third < nKT) { load(a, third); if (kAheadX) load_x(ax, third); }
+        multiply(b, bx);
+        kt = third;
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -118,7 +147,8 @@ npas_status linear_mx_gv_launch(const npas_mx_linear_desc &d, const void *x, int
 {
     if (!linear_mx_gv_supported(d)) return NPAS_ERR_UNSUPPORTED;
     const MxLayout L = mx_layout(d.O, d.I);
-    const int warps = L.nKT < kMaxWarps ? (int)L.nKT : kMaxWarps;
+    // sixteen warps where a block has an SM to itself, else eight, of which two blocks fit on one
+    const int most = (int)L.nRT * 4 <= sm_count() ? kMaxWarps : kMaxWarps / 2, warps = (int)L.nKT < most ? (int)L.nKT : most;
     const auto kernel = d.M <= 8 ? linear_mx_gv_kernel<1> : linear_mx_gv_kernel<2>;
     const cudaError_t e = launch_pdl(Launch(), kernel, dim3(L.nRT * 4), dim3((unsigned)(warps * 32)), 0, st, (int)d.M, (int)d.I, (int)d.O, (int)d.relu,
                                      (int)(d.y_dtype == NPAS_BF16), (int)L.nKT, L.pitch, L.off_scales, L.off_values, x_pitch, static_cast<const uint16_t *>(x),
