@@ -56,21 +56,22 @@ __device__ __forceinline__ void st_cluster_v4(uint32_t addr, uint32_t a, uint32_
 {
     asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-__device__ __forceinline__ float load_res(const void *res, int64_t at, int y_bf16)
+template <bool kBf16> __device__ __forceinline__ float load_res(const void *res, int64_t at)
 {
-    return y_bf16 ? bf16_bits_to_f32(__ldg(static_cast<const uint16_t *>(res) + at)) : __ldg(static_cast<const float *>(res) + at);
+    if constexpr (kBf16) return bf16_bits_to_f32(__ldg(static_cast<const uint16_t *>(res) + at));
+    else return __ldg(static_cast<const float *>(res) + at);
 }
-__device__ __forceinline__ void store_y(void *y, int64_t at, float v, int relu, int y_bf16)
+template <bool kBf16> __device__ __forceinline__ void store_y(void *y, int64_t at, float v, int relu)
 {
     if (relu) v = fmaxf(v, 0.f);
-    if (y_bf16) static_cast<uint16_t *>(y)[at] = (uint16_t)cvt_bf16x2(v, 0.f);
+    if constexpr (kBf16) static_cast<uint16_t *>(y)[at] = (uint16_t)cvt_bf16x2(v, 0.f);
     else static_cast<float *>(y)[at] = v;
 }
 
 // what the input is: a blob, 16 bits to be quantised, 16 bits
 enum MxIn { kBlob, kQuantize, kWide };
 
-template <MxIn kIn>
+template <MxIn kIn, bool kBf16>
 __global__ void __launch_bounds__(kThreads, 2)
 linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w, const MxSwParams p, const uint8_t *xin,
                     const uint8_t *wblob, const float *bias, const void *res, void *y, uint32_t *ws)
@@ -260,14 +261,20 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
                 __syncwarp();
                 tmem_ld_x16(t_addr + c0, v);
                 if (p.KS == 1) {
+                    const int64_t at = (int64_t)(mt * p.N + c0) * p.O + o + z;
+                    const int n = o < p.O ? rows - c0 : 0;
                     float add[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        add[i] = res && o < p.O && c0 + i < rows ? load_res(res, (int64_t)(mt * p.N + c0 + i) * p.O + o + z, p.y_bf16) : 0.f;
+                    for (int i = 0; i < 16; ++i) add[i] = 0.f;
+                    if (res) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (i < n) add[i] = load_res<kBf16>(res, at + (int64_t)i * p.O);
+                    }
                     tmem_ld_wait();
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (o < p.O && c0 + i < rows) store_y(y, (int64_t)(mt * p.N + c0 + i) * p.O + o, __uint_as_float(v[i]) + b + add[i], p.relu, p.y_bf16);
+                        if (i < n) store_y<kBf16>(y, at + (int64_t)i * p.O, __uint_as_float(v[i]) + b + add[i], p.relu);
                 } else {
                     // four rows of X at a time to the CTA that owns them: [rank][output][its rows] floats, an output's padded by 16 bytes
                     tmem_ld_wait();
@@ -301,7 +308,7 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
         const int64_t at = (int64_t)(mt * p.N + rank * p.cpr + m0) * p.O + o + z;
         float add[4], v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) add[j] = res && m0 + j < own ? load_res(res, at + (int64_t)j * p.O, p.y_bf16) : 0.f;
+        for (int j = 0; j < 4; ++j) add[j] = res && m0 + j < own ? load_res<kBf16>(res, at + (int64_t)j * p.O) : 0.f;
         const uint8_t *src = smem + p.off_red + (uint32_t)ol * p.red_pitch + (uint32_t)m0 * 4u;
         for (int s = 0; s < live; ++s, src += kRows * p.red_pitch) {
             const float4 u = *reinterpret_cast<const float4 *>(src);
@@ -310,8 +317,47 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
         const float b = bias ? __ldg(bias + o + z) : 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (m0 + j < own) store_y(y, at + (int64_t)j * p.O, v[j] + b + add[j], p.relu, p.y_bf16);
+            if (m0 + j < own) store_y<kBf16>(y, at + (int64_t)j * p.O, v[j] + b + add[j], p.relu);
     }
+}
+
+// the rest of the plan for a split into `ks`; false where shared or tensor memory does not hold it
+bool shape(MxSwParams &p, bool mx, int ks, int sms)
+{
+    p.KS = ks;
+    p.spr = (p.nS + ks - 1) / ks;
+    p.cpr = ((p.N + ks - 1) / ks + 3) / 4 * 4;
+    p.red_pitch = (uint32_t)p.cpr * 4u + 16u;
+    const uint32_t red = ks > 1 ? (uint32_t)ks * kRows * p.red_pitch : 0u;
+    const uint32_t fixed = red + (uint32_t)sizeof(MxSwBars) + 128u + 1024u;
+    p.x_bytes = (uint32_t)p.N * 128u;
+    p.stage_bytes = round_up(kWBytes + (mx ? 2 * kScaleBytes + p.x_bytes : kScaleBytes), 1024);
+    // (two CTAs on an SM where there are more CTAs than SMs)
+    const uint32_t limit = (long long)p.nMT * p.nOT * ks > sms ? kSmemHalf : kSmemLimit;
+    if (fixed >= limit) return false;
+    const uint32_t budget = limit - fixed;
+    p.SX = 0;
+    if (!mx) {
+        // the input's ring (of 64 columns a stage)
+        p.SX = kMaxXStages;
+        while (p.SX > 2 && (uint32_t)p.SX * p.x_bytes + 3 * p.stage_bytes > budget) --p.SX;
+        if ((uint32_t)p.SX * p.x_bytes >= budget) return false;
+    }
+    p.S = (int)((budget - (uint32_t)p.SX * p.x_bytes) / p.stage_bytes);
+    if (p.S > kMaxStages) p.S = kMaxStages;
+    if (p.S > p.spr) p.S = p.spr;
+    if (p.S < 1 || (p.S < 2 && p.spr > 1)) return false;
+    p.off_x = (uint32_t)p.S * p.stage_bytes;
+    p.off_red = p.off_x + (uint32_t)p.SX * p.x_bytes;
+    p.off_bar = round_up(p.off_red + red, 128);
+    p.smem_bytes = p.off_bar + (uint32_t)sizeof(MxSwBars) + 1024u;
+    if (p.smem_bytes > kSmemLimit) return false;
+    // columns of tensor memory: the sums, then scales of every stage (4-bit) or the widened weights
+    p.tmem_scales = round_up((uint32_t)p.N, 32);
+    const uint32_t cols = p.tmem_scales + (mx ? 16u * p.S : 32u * kSlots);
+    p.tmem_cols = 32;
+    while (p.tmem_cols < cols) p.tmem_cols *= 2;
+    return p.tmem_cols <= 512;
 }
 
 bool plan(const npas_mx_linear_desc &d, MxSwParams &p, int sms)
@@ -332,47 +378,10 @@ bool plan(const npas_mx_linear_desc &d, MxSwParams &p, int sms)
     // the clusters fill less than half the chip (more do not fit side by side: 32x2048 -> 2048 4.8 us in fours, 5.5 in eights)
     const long long tiles = (long long)p.nMT * p.nOT;
     if (tiles > 0x7FFFFFFF / kMaxSplit) return false;
-    p.KS = 1;
-    while (p.KS < kMaxSplit && 2 * p.KS <= p.nS && tiles * 2 * p.KS <= (2 * p.KS == 8 ? sms / 2 : mx ? sms : 2 * sms)) p.KS *= 2;
-    if (d.variant) {
-        p.KS = d.variant;
-        if (p.KS < 1 || p.KS > kMaxSplit || p.KS & (p.KS - 1)) return false;
-    }
-    p.spr = (p.nS + p.KS - 1) / p.KS;
-    p.cpr = ((p.N + p.KS - 1) / p.KS + 3) / 4 * 4;
-    p.red_pitch = (uint32_t)p.cpr * 4u + 16u;
-    const uint32_t red = p.KS > 1 ? (uint32_t)p.KS * kRows * p.red_pitch : 0u;
-    const uint32_t fixed = red + (uint32_t)sizeof(MxSwBars) + 128u + 1024u;
-    p.x_bytes = (uint32_t)p.N * 128u;
-    p.stage_bytes = round_up(kWBytes + (mx ? 2 * kScaleBytes + p.x_bytes : kScaleBytes), 1024);
-    // (two CTAs on an SM where there are more CTAs than SMs)
-    const uint32_t limit = tiles * p.KS > sms ? kSmemHalf : kSmemLimit;
-    if (fixed >= limit) return false;
-    const uint32_t budget = limit - fixed;
-    if (mx) {
-        p.S = (int)(budget / p.stage_bytes);
-        p.SX = 0;
-    } else {
-        // the input's ring (of 64 columns a stage)
-        p.SX = kMaxXStages;
-        while (p.SX > 2 && (uint32_t)p.SX * p.x_bytes + 3 * p.stage_bytes > budget) --p.SX;
-        if ((uint32_t)p.SX * p.x_bytes >= budget) return false;
-        p.S = (int)((budget - (uint32_t)p.SX * p.x_bytes) / p.stage_bytes);
-    }
-    if (p.S > kMaxStages) p.S = kMaxStages;
-    if (p.S > p.spr) p.S = p.spr;
-    if (p.S < 1 || (p.S < 2 && p.spr > 1)) return false;
-    p.off_x = (uint32_t)p.S * p.stage_bytes;
-    p.off_red = p.off_x + (uint32_t)p.SX * p.x_bytes;
-    p.off_bar = round_up(p.off_red + red, 128);
-    p.smem_bytes = p.off_bar + (uint32_t)sizeof(MxSwBars) + 1024u;
-    if (p.smem_bytes > kSmemLimit) return false;
-    // columns of tensor memory: the sums, then scales of every stage (4-bit) or the widened weights
-    p.tmem_scales = round_up((uint32_t)p.N, 32);
-    const uint32_t cols = p.tmem_scales + (mx ? 16u * p.S : 32u * kSlots);
-    p.tmem_cols = 32;
-    while (p.tmem_cols < cols) p.tmem_cols *= 2;
-    return p.tmem_cols <= 512;
+    if (d.variant) return d.variant >= 1 && d.variant <= kMaxSplit && !(d.variant & (d.variant - 1)) && shape(p, mx, d.variant, sms);
+    for (int ks = kMaxSplit; ks > 1; ks /= 2)
+        if (ks <= p.nS && tiles * ks <= (ks == 8 ? sms / 2 : mx ? sms : 2 * sms) && shape(p, mx, ks, sms)) return true;
+    return shape(p, mx, 1, sms);
 }
 
 bool planned(const npas_mx_linear_desc &d, MxSwParams &p)
@@ -401,7 +410,9 @@ npas_status linear_mx_sw_launch(const npas_mx_linear_desc &d, const void *x, int
     else if (!(blob ? mx_encode_values(&tmx, x, mx_layout(d.M, d.I), d.M, (uint32_t)p.N)
                     : mx_encode_bf16(&tmx, x, (uint64_t)d.I, (uint64_t)x_pitch, (uint64_t)d.M, (uint32_t)p.N)))
         return NPAS_ERR_CUDA;
-    const auto kernel = blob ? linear_mx_sw_kernel<kBlob> : d.quantize_x ? linear_mx_sw_kernel<kQuantize> : linear_mx_sw_kernel<kWide>;
+    const auto kernel = blob ? (p.y_bf16 ? linear_mx_sw_kernel<kBlob, true> : linear_mx_sw_kernel<kBlob, false>)
+                      : d.quantize_x ? (p.y_bf16 ? linear_mx_sw_kernel<kQuantize, true> : linear_mx_sw_kernel<kQuantize, false>)
+                                     : (p.y_bf16 ? linear_mx_sw_kernel<kWide, true> : linear_mx_sw_kernel<kWide, false>);
     if (allow_dynamic_smem(reinterpret_cast<const void *>(kernel), (int)kSmemLimit) != NPAS_OK) return NPAS_ERR_CUDA;
     const dim3 grid((unsigned)(p.nMT * p.nOT * p.KS)), block(kThreads);
     const uint8_t *xb = static_cast<const uint8_t *>(x), *wb = static_cast<const uint8_t *>(w);

@@ -48,12 +48,47 @@ struct MxWalk {
 
 struct MxEpiBars {
     uint64_t acc_full[2], acc_empty[2];
-    uint64_t slab_ready[kMxMaxSlabs], slab_done[kMxMaxSlabs];  // free (or its residuals have landed) / every epilogue warp has finished its part
+    uint64_t landed[kMxMaxSlabs], slab_done[kMxMaxSlabs];      // a slab's residuals have landed / its epilogue warps have finished their parts
+    uint32_t freed;                                            // slabs, in their order, that have left: number n may be written when n - NS has
 };
+
+// Bounded wait for the count of slabs that have left.  (A count and not a barrier's parity: a warp has a part in some uses of a slab only, and
+// could find the parity of the use before last.)
+__device__ __forceinline__ bool mx_wait_freed(const MxEpiBars *bars, uint32_t n, volatile uint32_t *abort_flag, uint32_t *ws, uint32_t where)
+{
+    auto ready = [&]() {
+        uint32_t v;
+        asm volatile("ld.acquire.cta.shared::cta.u32 %0, [%1];" : "=r"(v) : "r"(smem_u32(&bars->freed)) : "memory");
+        return (int32_t)(v - n) >= 0;
+    };
+    if (ready()) return true;
+    long long t0 = 0;
+    uint32_t spins = 0;
+    while (!ready()) {
+        __nanosleep(32);
+        ++spins;
+        if (spins == 256u) t0 = clock64();
+        else if ((spins & 255u) == 0u) {
+            if (*abort_flag) return false;
+            if (clock64() - t0 > kWaitLimitCycles) {
+                *abort_flag = 1;
+                if (atomicCAS(ws, 0u, 10u /* NPAS_ERR_TIMEOUT */) == 0u) ws[1] = where;
+                return false;
+            }
+        }
+    }
+    return true;
+}
+__device__ __forceinline__ void mx_set_freed(MxEpiBars *bars, uint32_t n)
+{
+    asm volatile("st.release.cta.shared::cta.u32 [%0], %1;" ::"r"(smem_u32(&bars->freed)), "r"(n) : "memory");
+}
+
 __device__ __forceinline__ void mx_epi_init(MxEpiBars *bars, const MxTiles &p, int releases)
 {
     for (int a = 0; a < 2; ++a) { mbar_init(&bars->acc_full[a], 1); mbar_init(&bars->acc_empty[a], releases); }
-    for (int n = 0; n < p.NS; ++n) { mbar_init(&bars->slab_ready[n], 1); mbar_init(&bars->slab_done[n], 4); }
+    for (int n = 0; n < p.NS; ++n) { mbar_init(&bars->landed[n], 1); mbar_init(&bars->slab_done[n], 4); }
+    bars->freed = 0;
 }
 
 // ---- the slabs' copies, one thread: a slab leaves by TMA as soon as every epilogue warp has finished its part; when the store before it has
@@ -84,7 +119,7 @@ __device__ __forceinline__ void mx_slab_copies(const MxTiles &p, int unit, int r
 {
     const uint32_t mask = (uint32_t)p.NS - 1;
     auto request = [&](const MxSlabWalk &w, uint32_t n) {
-        uint64_t *bar = &bars->slab_ready[n & mask];
+        uint64_t *bar = &bars->landed[n & mask];
         mbar_arrive_expect_tx(bar, kMxSlabBytes);
         tma_load_2d(smem + p.off_slabs + (size_t)(n & mask) * kMxSlabBytes, tmap_r, bar, w.t.o0(p) + w.h * 64, w.t.m0(p) + w.r * 128);
     };
@@ -97,8 +132,8 @@ __device__ __forceinline__ void mx_slab_copies(const MxTiles &p, int unit, int r
         bulk_commit();
         if (n) {
             bulk_wait_read<1>();
-            if (!res) mbar_arrive(&bars->slab_ready[(n - 1) & mask]);
-            else if (ahead.in(p)) { request(ahead, asked++); ahead.next(p); }             // (slab n - 1 + NS)
+            mx_set_freed(bars, n);
+            if (res && ahead.in(p)) { request(ahead, asked++); ahead.next(p); }           // (slab n - 1 + NS)
         }
     }
     bulk_wait_read<0>();                                       // the slabs stay valid until the last store has read them
@@ -153,12 +188,12 @@ __device__ __forceinline__ void mx_epilogue_slabs(const MxTiles &p, int unit, in
                 if (p.relu) h[i] = relu_bf16x2(h[i]);
             }
         };
-        // the slab of block r, ready for this warp.  With residuals: they have landed; without: the store that last used the slab has read
-        // it (from its second use on)
+        // the slab of block r: what last lay in it has left, and with residuals, they have landed
         auto slab_of = [&](int r, uint32_t &slot) {
-            const uint32_t at = n_tile + (uint32_t)(r * halves + half), use = at >> p.ns_log;
+            const uint32_t at = n_tile + (uint32_t)(r * halves + half);
             slot = at & (p.NS - 1);
-            return !(res || use) || __all_sync(0xFFFFFFFFu, mbar_wait(&bars->slab_ready[slot], (res ? use : use - 1) & 1u, abort_flag, ws, 0xC510));
+            return __all_sync(0xFFFFFFFFu, (at < (uint32_t)p.NS || mx_wait_freed(bars, at - p.NS + 1, abort_flag, ws, 0xC510)) &&
+                                               (!res || mbar_wait(&bars->landed[slot], (at >> p.ns_log) & 1u, abort_flag, ws, 0xC511)));
         };
         auto hand_over = [&](uint32_t slot) {
             fence_proxy_async_smem();                          // the TMA store reads what this thread wrote

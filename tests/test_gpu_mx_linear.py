@@ -268,3 +268,32 @@ def test_refusals():
         assert e.value.code == code, bad
     with pytest.raises(TypeError):
         npas.linear_mx(x, w, out_dtype=torch.float16)
+
+
+@pytest.mark.parametrize("kind", ["blob", "16"])
+@pytest.mark.parametrize("path,variant", [(4, 128), (4, 256), (5, 0)])
+@pytest.mark.parametrize("M,I,O,res", [(1939, 585, 3768, False), (2500, 2112, 128, True), (4867, 640, 560, True), (1300, 2304, 3128, True), (9000, 64, 328, False),
+                                       (20000, 40, 72, True)])
+def test_outputs_that_end_inside_a_tile_many_times(M, I, O, res, path, variant, kind):
+    """Tiles with one half of 64 outputs between tiles with two, blocks of rows that end inside a tile: the order of the slabs shifts
+    between the warps that fill them.  Every run has to give the same bits."""
+    if path == 5 and kind == "16":
+        pytest.skip("4-bit inputs only")
+    c = _case(M, I, O, seed=31, res=res)
+    x, w = c["x"].cuda(), npas.quantize_mx(c["w"].cuda())
+    x = npas.quantize_mx(x) if kind == "blob" else x
+    bias, r = c["bias"].cuda(), c["res"].cuda() if res else None
+    ws = npas.linear_mx_workspace(M, w, dtype="mx" if kind == "blob" else torch.bfloat16, path=path, variant=variant)
+    f = lambda: npas.linear_mx(x, w, bias, r, relu=True, ws=ws, path=path, variant=variant)
+    y = f()
+    npas.check_device_status(ws)
+    xv = npas.dequantize_mx(x, torch.float32) if kind == "blob" else x.float()
+    wv = npas.dequantize_mx(w, torch.float32)
+    ref = xv.double() @ wv.double().T + bias.double() + (r.double() if res else 0)
+    size = xv.abs().double() @ wv.abs().double().T + bias.abs().double() + (r.abs().double() if res else 0)
+    off = (I + 3) * 2.0 ** -23 * size
+    over = (y.double() - ref.relu()).abs() - (off + 2.0 ** -8 * (ref.abs() + off))
+    assert float(over.max()) <= 0
+    for _ in range(30):
+        assert torch.equal(f(), y)
+    npas.check_device_status(ws)
