@@ -20,8 +20,8 @@ npas_status check_args(const npas_mx_linear_desc *d)
     return NPAS_OK;
 }
 
-// 1: CUDA cores, 3: few rows, 4: persistent tiles, 5: the same on CTA pairs, 6: a 16-bit input of up to 16 rows.  0: the requested path does not take the geometry.
-// Up to 16 rows the kernel for few rows quantises the input itself: every CTA its share, again for every 128 outputs.  (FIXME)
+// Up to 16 rows the kernel for few rows quantises the input itself: every CTA its share, again for every 128 outputs.  One launch less
+// (1x2048 -> 1000 6.0 -> 4.2 us of host time); from 32 rows on its CTAs take longer than the launch (32x2048 -> 2048 6.8 us, 6.3 in two).
 bool quantizes_itself(const npas_mx_linear_desc &d) { return d.quantize_x && d.M <= 16; }
 
 npas_mx_linear_desc behind_quantize(npas_mx_linear_desc d)
@@ -30,23 +30,83 @@ npas_mx_linear_desc behind_quantize(npas_mx_linear_desc d)
     return d;
 }
 
-int kernel_for(const npas_mx_linear_desc &d)
+// Kernel (1: CUDA cores, 3: few rows, 4: persistent tiles, 5: the same on CTA pairs, 6: a 16-bit input of up to 16 rows; 0: none) and variant.
+struct Choice { int kernel, variant; };
+
+// The automatic choice: the kernel, tile or split that a model puts lowest.  Fitted by least squares to 25 000 random layers per kind of input
+// (M 17 to 60000, I and O 16 to 8192, a third with residuals, half of odd widths), each timed on every kernel that takes it: standard
+// error 8 to 16 %, the kernel it picks takes 1.4 % (4-bit) and 2 % (16-bit) more than the best one on average.  Microseconds of a launch,
+// and per round of tiles of a stage of 256 columns (of a step of 64 with a 16-bit input; where the weights stay), of the epilogue, of
+// residuals in slabs, of bf16 outputs that do not leave by TMA, of those with residuals, of fp32 residuals.
+struct Cost { double launch, k, k_stay, round, res, direct, direct_res, f32_res; };
+constexpr Cost kCosts[2][3] = {
+    {{3.66, 0.463, 0.467, 0.72, 0.35, 0.02, 1.30, 0.34}, {2.73, 0.555, 0.738, 2.12, 0.58, 0.05, 1.35, 0.22}, {2.13, 0.359, 0.359, 3.19, 0.64, 0.22, 2.08, 0.47}},
+    {{3.68, 0.268, 0.156, 1.32, 0.33, 0.32, 1.67, 0.43}, {2.84, 0.322, 0.353, 2.73, 0.70, 0.56, 2.18, 0.23}, {}}};
+
+Choice choose(const npas_mx_linear_desc &d)
+{
+    const npas_mx_linear_desc in = behind_quantize(d);
+    const bool mx = in.x_dtype == NPAS_MX4;
+    const int sms = sm_count();
+    const auto div = [](long long a, long long b) { return (a + b - 1) / b; };
+    const long long stages = div(d.I, 256), steps = div(d.I, 64);
+    Choice best = {0, 0};
+    double least = 0.;
+    auto consider = [&](int kernel, int variant, double us) {
+        npas_mx_linear_desc t = in;
+        t.variant = variant;
+        if (best.kernel && us >= least) return;
+        if (kernel == 3 ? !linear_mx_sw_supported(t) : kernel == 4 ? !linear_mx_ps_supported(t) : !linear_mx_d2_supported(t)) return;
+        best = {kernel, variant}; least = us;
+    };
+    // (a few rows more than eight of few columns are left to the tensor cores: 14x48 -> 1042 4.2 us against 3.7)
+    if (linear_mx_gv_supported(in) && (d.M <= 8 || d.I > 128)) return {6, 0};
+    // few rows: a CTA, or a cluster that splits the columns, per 128 outputs and up to 128 rows
+    if (d.M <= 1024) {
+        const long long tiles = div(d.M, 128) * div(d.O, 128);
+        const double rows = d.M < 128 ? (double)div(d.M, 16) * 16. : 128.;
+        for (int ks = 1; ks <= 8; ks *= 2) {
+            // (a split is one wave; clusters do not straddle groups of SMs, so larger ones fill less of the chip: 34 of four took two waves)
+            if (ks > 1 && (ks > stages || tiles * ks > (ks == 8 ? sms / 2 : ks == 4 ? sms - sms / 9 : sms))) break;
+            const double us = (ks == 1 ? 2.8 : mx ? 2.9 : 3.4) + (double)div(tiles * ks, sms) * ((mx ? 0.306 : 1.04) * (double)div(stages, ks) +
+                                                                (ks == 1 ? 0.019 : 0.039) * rows + (d.has_residual ? (ks == 1 ? 0.031 : 0.004) * rows : 0.));
+            consider(3, ks, us);
+        }
+        if (quantizes_itself(d)) return best;
+    }
+    // persistent tiles of 128 or 256 rows, and of 256 on CTA pairs
+    const bool f32 = d.y_dtype == NPAS_F32, direct = !f32 && d.O % 8 != 0;
+    for (int i = 0; i < (mx && d.I >= 1024 && d.O > 128 ? 3 : 2); ++i) {
+        const Cost &c = kCosts[mx ? 0 : 1][i];
+        const bool pair = i == 2;
+        const long long across = div(d.O, pair ? 256 : 128), tiles = div(d.M, i == 0 ? 128 : 256) * across, units = pair ? sms / 2 : sms;
+        const bool stay = !pair && tiles > sms && sms / across * across * 8 >= sms * 7 && (mx ? stages <= 4 : steps <= 8);
+        const double rounds = (double)div(tiles, stay ? units / across * across : units), k = (double)(mx ? stages : steps);
+        consider(pair ? 5 : 4, pair ? 0 : i == 0 ? 128 : 256,
+                 c.launch + rounds * (k * (stay ? c.k_stay : c.k) + c.round + (direct ? c.direct : 0.) +
+                                      (d.has_residual ? direct ? c.direct_res : f32 ? c.f32_res : c.res : 0.)));
+    }
+    return best;
+}
+
+Choice choice_for(const npas_mx_linear_desc &d)
 {
     const npas_mx_linear_desc in = behind_quantize(d);
     switch (d.path) {
-        case 1: return d.variant ? 0 : 1;
-        case 3: return linear_mx_sw_supported(in) ? 3 : 0;
-        case 4: return linear_mx_ps_supported(in) ? 4 : 0;
-        case 5: return linear_mx_d2_supported(in) ? 5 : 0;
-        case 6: return linear_mx_gv_supported(in) ? 6 : 0;
+        case 1: return {d.variant ? 0 : 1, 0};
+        case 3: return {linear_mx_sw_supported(in) ? 3 : 0, d.variant};
+        case 4: return {linear_mx_ps_supported(in) ? 4 : 0, d.variant};
+        case 5: return {linear_mx_d2_supported(in) ? 5 : 0, d.variant};
+        case 6: return {linear_mx_gv_supported(in) ? 6 : 0, d.variant};
         case 0: case 2: break;
-        default: return 0;
+        default: return {0, 0};
     }
-    if (linear_mx_gv_supported(in)) return 6;
-    if (d.M > 128 && d.O > 128 && d.I >= 2048 && linear_mx_d2_supported(in)) return 5;
-    if (d.M > 128 && linear_mx_ps_supported(in)) return 4;
-    if (linear_mx_sw_supported(in)) return 3;
-    return d.path == 2 ? 0 : 1;
+    if (d.variant) return {0, 0};
+    Choice c = {0, 0};
+    const int32_t none = 0;
+    cached_plan(d, none, 0, c, [&](Choice &q) { q = choose(d); return true; });
+    if (!c.kernel && d.path == 0) c.kernel = 1;
+    return c;
 }
 
 // Rows of a 16-bit input that do not start on 16-byte boundaries are copied to a pitch that does: the tensor cores' kernels load by TMA.
@@ -56,7 +116,7 @@ int64_t pitch_of(const npas_mx_linear_desc &d) { return ((int64_t)d.I + 7) / 8 *
 // scratch behind the status words: the quantised input, or the copied one
 size_t scratch_bytes(const npas_mx_linear_desc &d)
 {
-    const int kernel = kernel_for(d);
+    const int kernel = choice_for(d).kernel;
     if (d.quantize_x) return kernel == 3 && quantizes_itself(d) ? 0 : mx_layout(d.M, d.I).total;
     return needs_pitch(d, kernel) ? (size_t)d.M * pitch_of(d) * 2 : 0;
 }
@@ -110,7 +170,7 @@ npas_status npas_linear_mx_kernel(const npas_mx_linear_desc *d, int32_t *kernel_
     if (!kernel_id) return NPAS_ERR_NULL;
     npas_status s = check_args(d);
     if (s != NPAS_OK) return s;
-    *kernel_id = kernel_for(*d);
+    *kernel_id = choice_for(*d).kernel;
     return *kernel_id ? NPAS_OK : NPAS_ERR_UNSUPPORTED;
 }
 
@@ -133,11 +193,13 @@ npas_status npas_internal_linear_mx(const npas_mx_linear_desc *d, const void *x,
     for (const void *q : {x, w, static_cast<const void *>(y), static_cast<const void *>(ws), res, static_cast<const void *>(bias)})
         if (q && !aligned16(q)) return NPAS_ERR_ALIGNMENT;
     if (x == y || w == y || res == y) return NPAS_ERR_UNSUPPORTED;
-    const int kernel = kernel_for(*d);
+    const Choice choice = choice_for(*d);
+    const int kernel = choice.kernel;
     if (!kernel) return NPAS_ERR_UNSUPPORTED;
     if (scratch_size < scratch_bytes(*d)) return NPAS_ERR_BUFFER_TOO_SMALL;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     npas_mx_linear_desc in = *d;
+    in.variant = choice.variant;
     if (d->quantize_x && !(kernel == 3 && quantizes_itself(*d))) {
         const npas_mx_desc q = {d->M, d->I, NPAS_BF16};
         s = quantize_mx_launch(q, x, scratch, st, Launch());

@@ -262,8 +262,8 @@ bool plan(const npas_mx_linear_desc &d, MxD2Params &p, int sms)
     mx_tiles_plan(p.t, d, kN, 2 * kRows, 1, sms / 2);
     if (!p.t.n_tiles) return false;
     p.w_scales = LW.off_scales; p.x_scales = LX.off_scales; p.w_tiles = (int)LW.nRT; p.x_tiles = (int)LX.nRT;
-    p.t.NS = !p.y_bf16 || d.O % 8 ? 0 : 2;
-    p.t.ns_log = 1;
+    p.t.NS = !p.y_bf16 || d.O % 8 ? 0 : d.has_residual ? 4 : 2;
+    p.t.ns_log = p.t.NS == 4 ? 2 : 1;
     const uint32_t fixed = (uint32_t)p.t.NS * kMxSlabBytes + 2 * kGroupBytes + (uint32_t)sizeof(MxD2Bars) + 1024u;
     p.S = (int)((kSmemLimit - fixed) / kStageBytes);
     if (p.S > kMaxStages) p.S = kMaxStages;

@@ -262,8 +262,7 @@ bool plan(const npas_mx_linear_desc &d, MxPsParams &p, int sms)
     p.y_bf16 = d.y_dtype == NPAS_BF16;
     p.nS = (d.I + kStepCols - 1) / kStepCols;
     p.nKT = (int)LW.nKT;
-    const int want = d.variant & 0xFFFF;
-    const int N = want ? want : d.I >= 2048 && (long long)((d.M + 255) / 256) * ((d.O + 127) / 128) >= sms ? 256 : 128;
+    const int N = d.variant & 0xFFFF ? d.variant & 0xFFFF : 128;              // (the automatic choice names a width)
     if ((N != 128 && N != 256) || d.variant >> 17) return false;
     mx_tiles_plan(p.t, d, N, kRows, N == 128 ? 2 : 1, sms);
     if (!p.t.n_tiles) return false;
@@ -278,9 +277,9 @@ bool plan(const npas_mx_linear_desc &d, MxPsParams &p, int sms)
     p.off_stages = mx && p.resident ? (uint32_t)p.nS * kWStage : 0u;
     p.stage_bytes = p.x_in_stage + (mx ? p.xs_bytes + p.x_bytes : 0u);
     const uint32_t budget = kSmemLimit - (uint32_t)sizeof(MxPsBars) - 128u - 1024u;
-    // Slabs for bf16 outputs with rows on 16-byte boundaries: two where the loads need the room (256 rows of X), else four, eight where
+    // Slabs for bf16 outputs with rows on 16-byte boundaries: two where the loads need the room (256 rows of X, no residuals), else four, eight where
     // residuals are ahead of little else; and the input's ring
-    p.t.NS = !p.y_bf16 || d.O % 8 ? 0 : N == 256 && p.nS > 2 ? 2 : mx && d.has_residual && p.nS <= 2 && N == 128 ? 8 : 4;
+    p.t.NS = !p.y_bf16 || d.O % 8 ? 0 : N == 256 && p.nS > 2 && !d.has_residual ? 2 : mx && d.has_residual && p.nS <= 2 && N == 128 ? 8 : 4;
     while ((1 << p.t.ns_log) < p.t.NS) ++p.t.ns_log;
     p.slots = mx ? 0 : p.resident ? nK : kSlots;
     if (!mx) p.SX = N == 256 ? (p.t.NS == 4 ? 3 : 4) : 6;

@@ -374,14 +374,10 @@ bool plan(const npas_mx_linear_desc &d, MxSwParams &p, int sms)
     // Input rows of a tile: all of them, or equal shares in multiples of 16 (4-bit: a tile starts where a tile of scales does)
     p.N = mx && p.nMT > 1 ? kRows : ((d.M + p.nMT - 1) / p.nMT + 15) / 16 * 16;
     p.w_scales = LW.off_scales; p.x_scales = LX.off_scales;
-    // Split of the columns: up to a CTA per SM, two where weights are widened (which takes longer than they take to arrive); eight only while
-    // the clusters fill less than half the chip (more do not fit side by side: 32x2048 -> 2048 4.8 us in fours, 5.5 in eights)
     const long long tiles = (long long)p.nMT * p.nOT;
     if (tiles > 0x7FFFFFFF / kMaxSplit) return false;
     if (d.variant) return d.variant >= 1 && d.variant <= kMaxSplit && !(d.variant & (d.variant - 1)) && shape(p, mx, d.variant, sms);
-    for (int ks = kMaxSplit; ks > 1; ks /= 2)
-        if (ks <= p.nS && tiles * ks <= (ks == 8 ? sms / 2 : mx ? sms : 2 * sms) && shape(p, mx, ks, sms)) return true;
-    return shape(p, mx, 1, sms);
+    return shape(p, mx, 1, sms);                               // (the automatic choice names a split)
 }
 
 bool planned(const npas_mx_linear_desc &d, MxSwParams &p)

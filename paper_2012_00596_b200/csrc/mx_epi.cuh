@@ -285,6 +285,8 @@ __device__ __forceinline__ void mx_store_rows(const uint32_t (&v)[32], const flo
         asm volatile("" : "+l"(q));
     }
 }
+__device__ __forceinline__ void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
 template <int kGroups, bool kBf16, typename F>
 __device__ __forceinline__ void mx_epilogue_rows(const MxTiles &p, int unit, int rank, int e, int lane, int quarter, uint32_t tmem_base, MxEpiBars *bars, const float *bias,
                                                  const void *res, void *y, volatile uint32_t *abort_flag, uint32_t *ws, F release)
@@ -296,6 +298,25 @@ __device__ __forceinline__ void mx_epilogue_rows(const MxTiles &p, int unit, int
         const int o = w.o0(p) + quarter * 32 + lane, blocks = w.blocks(p);
         const uint32_t acc = p.acc == 2 ? it & 1u : 0u, lap = p.acc == 2 ? it >> 1 : it;
         const float b = bias && o < p.O ? __ldg(bias + o) : 0.f;
+        if (res) {
+            // the residuals of this warp's next tile on their way to L2 (fetched when they are needed they held the tile up twice)
+            MxWalk next = w;
+            next.next(p);
+            if (p.acc == 2 && kGroups == 2) next.next(p);
+            const int no = next.o0(p) + quarter * 32;
+            if (next.in(p) && no < p.O)
+                for (int r = p.acc == 1 && kGroups == 2 ? group : 0; r < next.blocks(p); r += step)
+#pragma unroll
+                    for (int c = 0; c < 64; c += 32) {
+                        const int m = next.m0(p) + r * 128 + part * 64 + c + lane;
+                        if (m >= p.M) continue;
+                        constexpr int kSize = kBf16 ? 2 : 4;
+                        const char *q = static_cast<const char *>(res) + ((int64_t)m * p.O + no) * kSize, *last = q + (min(32, p.O - no) * kSize - 1);
+#pragma unroll
+                        for (int i = 0; i < 32 * kSize; i += 32) prefetch_l2(q + i < last ? q + i : last);
+                        prefetch_l2(last);
+                    }
+        }
         bool waited = false;
         for (int r = p.acc == 1 && kGroups == 2 ? group : 0; r < blocks; r += step)
             for (int c = 0; c < 64; c += 32) {

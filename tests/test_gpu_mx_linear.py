@@ -270,15 +270,12 @@ def test_refusals():
         npas.linear_mx(x, w, out_dtype=torch.float16)
 
 
-@pytest.mark.parametrize("kind", ["blob", "16"])
-@pytest.mark.parametrize("path,variant", [(4, 128), (4, 256), (5, 0)])
+@pytest.mark.parametrize("kind,path,variant", [("blob", 4, 128), ("blob", 4, 256), ("blob", 5, 0), ("16", 4, 128), ("16", 4, 256)])
 @pytest.mark.parametrize("M,I,O,res", [(1939, 585, 3768, False), (2500, 2112, 128, True), (4867, 640, 560, True), (1300, 2304, 3128, True), (9000, 64, 328, False),
                                        (20000, 40, 72, True)])
-def test_outputs_that_end_inside_a_tile_many_times(M, I, O, res, path, variant, kind):
+def test_outputs_that_end_inside_a_tile_many_times(M, I, O, res, kind, path, variant):
     """Tiles with one half of 64 outputs between tiles with two, blocks of rows that end inside a tile: the order of the slabs shifts
     between the warps that fill them.  Every run has to give the same bits."""
-    if path == 5 and kind == "16":
-        pytest.skip("4-bit inputs only")
     c = _case(M, I, O, seed=31, res=res)
     x, w = c["x"].cuda(), npas.quantize_mx(c["w"].cuda())
     x = npas.quantize_mx(x) if kind == "blob" else x
@@ -294,6 +291,6 @@ def test_outputs_that_end_inside_a_tile_many_times(M, I, O, res, path, variant, 
     off = (I + 3) * 2.0 ** -23 * size
     over = (y.double() - ref.relu()).abs() - (off + 2.0 ** -8 * (ref.abs() + off))
     assert float(over.max()) <= 0
-    for _ in range(30):
+    for _ in range(20):
         assert torch.equal(f(), y)
     npas.check_device_status(ws)
