@@ -143,9 +143,17 @@ linear_mx_d2_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
                     const uint32_t st = base + s * kStageBytes, a_lo = ((st + kXBytes) >> 4) | kMxDescLboOne, b_lo = (st >> 4) | kMxDescLboOne;
                     const uint32_t sf = tmem_base + kTmemScales + ((g & 1) * kGroup + in_group) * kScaleCols;
                     const int n = min(4, nK - 4 * step);
-                    for (int j = 0; j < n; ++j)                                      // 64 columns = 32 bytes inside the swizzled row
-                        mma_mxf4_ss_pair(tmem_base, mx_desc64(a_lo + 2 * j), mx_desc64(b_lo + 2 * j), j & 1 ? idesc1 : idesc0, sf + 4 * (j / 2), sf + 8 + 8 * (j / 2),
-                                         step > 0 || j > 0);
+                    uint32_t more = step > 0;
+                    auto mma = [&](uint32_t j) {                                     // 64 columns = 32 bytes inside the swizzled row
+                        mma_mxf4_ss_pair(tmem_base, mx_desc64(a_lo + 2 * j), mx_desc64(b_lo + 2 * j), j & 1 ? idesc1 : idesc0, sf + 4 * (j / 2), sf + 8 + 8 * (j / 2), more);
+                        more = 1;
+                    };
+                    if (n == 4) { mma(0); mma(1); mma(2); mma(3); }                  // (no branch between the MMAs of a whole stage)
+                    else {
+                        mma(0);
+                        if (n > 1) mma(1);
+                        if (n > 2) mma(2);
+                    }
                     mma_commit_pair(&bars->empty[s]);
                     if (in_group == kGroup - 1 || step + 1 == p.nS) { mma_commit_pair(&bars->scales_empty[g & 1]); ++g; }
                     if (++s == (uint32_t)p.S) { s = 0; ph ^= 1u; }

@@ -18,7 +18,8 @@ namespace {
 
 constexpr int kRows = 128;
 constexpr int kStepCols = 256;                             // columns of a weight stage
-constexpr int kMaxStages = 6, kMaxXStages = 8, kSlots = 4, kMaxSlots = 8;
+constexpr int kMaxStages = 6, kMaxXStages = 4, kSlots = 4;
+constexpr uint32_t kSlotCols = 64;                         // tensor memory of a slot: 128 widened columns of the weights
 constexpr uint32_t kSmemLimit = 232448;
 constexpr uint32_t kWBytes = kRows * 128;
 constexpr uint32_t kScaleBytes = 2 * kMxScaleTile;         // of 128 rows and a stage
@@ -35,7 +36,7 @@ template <bool kMx> struct Roles {
 
 struct MxPsParams {
     MxTiles t;
-    int I, nS, nKT, S, SX, slots, resident;                    // SX: stages of the input (16 bits); slots: of widened weights; resident: weights stay
+    int I, nS, nKT, S, SX, x_steps, slots, resident;           // SX: stages of a 16-bit input, of x_steps K steps; slots: of widened weights; resident: weights stay
     uint32_t x_bytes, xs_bytes, stage_bytes, x_in_stage, off_stages, off_x, off_bar, smem_bytes, tmem_cols, tmem_scales, scale_cols;
     uint64_t w_scales, x_scales;                           // offsets of the scales in the blobs
     int y_bf16;
@@ -44,7 +45,7 @@ struct MxPsParams {
 struct MxPsBars {
     uint64_t full[kMaxStages], empty[kMaxStages];
     uint64_t x_full[kMaxXStages], x_empty[kMaxXStages];
-    uint64_t slot_full[kMaxSlots], slot_empty[kMaxSlots];
+    uint64_t slot_full[kSlots], slot_empty[kSlots];
     uint64_t w_full;                                       // resident weights of a 4-bit input
     MxEpiBars epi;
     uint32_t tmem_base;
@@ -128,6 +129,7 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
             uint32_t s = 0, ph = 0, it = 0, slot = 0, slot_ph = 0;
             bool ok = true;
             // tensor memory of scales: two tiles of W's a stage (a step where they stay), then X's, a K tile's row tiles side by side
+            const uint32_t idesc0 = idesc_mxf4(128, (uint32_t)p.t.N, 0), idesc1 = idesc_mxf4(128, (uint32_t)p.t.N, 1);
             const uint32_t xc = (uint32_t)p.t.N / 32, w_cols = kMx && p.resident ? 8u * p.nS : 0u;
             if (kMx && p.resident) {
                 ok = mbar_wait(&bars->w_full, 0, abort_flag, ws, 0xB330);
@@ -149,31 +151,77 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
                         const uint32_t sx = tmem_base + p.tmem_scales + w_cols + s * p.scale_cols + (p.resident ? 0u : 8u);
                         const uint32_t sw = p.resident ? tmem_base + p.tmem_scales + 8 * step : sx - 8u;
                         const int n = min(4, nK - 4 * step);
-                        for (int t = 0; t < (n + 1) / 2; ++t) {
-                            if (!p.resident) copy_scales(sw + 4 * t, wst + kWBytes + t * kMxScaleTile);
-                            for (int r = 0; r < p.t.N / kRows; ++r) copy_scales(sx + xc * t + 4 * r, xs + r * kScaleBytes + t * kMxScaleTile);
+                        const uint32_t ws_at = wst + kWBytes, wide = (uint32_t)p.t.N / kRows - 1u;
+                        uint32_t more = step > 0;
+                        // 128 columns: their scales, two MMAs of 64 columns (32 bytes inside the swizzled row); no branch between the MMAs of a
+                        // whole stage
+                        auto scales = [&](uint32_t t) {
+                            if (!p.resident) copy_scales(sw + 4 * t, ws_at + t * kMxScaleTile);
+                            copy_scales(sx + xc * t, xs + t * kMxScaleTile);
+                            if (wide) copy_scales(sx + xc * t + 4, xs + kScaleBytes + t * kMxScaleTile);
+                        };
+                        auto mma = [&](uint32_t j) {
+                            mma_mxf4_ss(d_tmem, mx_desc64(a_lo + 2 * j), mx_desc64(b_lo + 2 * j), j & 1 ? idesc1 : idesc0, sw + 4 * (j / 2), sx + xc * (j / 2), more);
+                            more = 1;
+                        };
+                        scales(0);
+                        if (n > 2) scales(1);
+                        if (n == 4) { mma(0); mma(1); mma(2); mma(3); }
+                        else {
+                            mma(0);
+                            if (n > 1) mma(1);
+                            if (n > 2) mma(2);
                         }
-                        for (int j = 0; j < n; ++j)                                  // 64 columns = 32 bytes inside the swizzled row
-                            mma_mxf4_ss(d_tmem, mx_desc64(a_lo + 2 * j), mx_desc64(b_lo + 2 * j), idesc_mxf4(128, (uint32_t)p.t.N, j & 1),
-                                        sw + 4 * (j / 2), sx + xc * (j / 2), step > 0 || j > 0);
                         mma_commit(&bars->empty[s]);
                         if (++s == (uint32_t)p.S) { s = 0; ph ^= 1u; }
                     }
                 } else {
-                    const uint32_t idesc = idesc_bf16_f32(128, (uint32_t)p.t.N), xb = base + p.off_x;
-                    for (int k = 0; k < nK; ++k) {
-                        // (weights that stay are waited for once: slot k holds step k)
-                        if (!mbar_wait(&bars->x_full[s], ph, abort_flag, ws, 0xB310) ||
-                            (!(p.resident && it > 0) && !mbar_wait(&bars->slot_full[slot], slot_ph, abort_flag, ws, 0xB320))) { ok = false; break; }
-                        tc_fence_after_sync();
-                        const uint32_t b_lo = ((xb + s * p.x_bytes) >> 4) | kMxDescLboOne, a_t = tmem_base + p.tmem_scales + slot * 32u;
+                    // The issuing thread's own instructions are on the critical path.  With 128 rows of X, waits and commits for every K step took it
+                    // 455 cycles a step while the MMAs take 256: there a slot's two steps are one stage of X, eight MMAs without a branch
+                    // between them (8192x4096 -> 4096 276 -> FIXME us).  With 256 rows the MMAs take 512, and stages of one step keep more
+                    // of X on its way.
+                    const uint32_t idesc = idesc_bf16_f32(128, (uint32_t)p.t.N), x16 = p.x_bytes >> 4, xb = ((base + p.off_x) >> 4) | kMxDescLboOne;
+                    const bool wait_w = !(p.resident && it > 0);                 // (weights that stay are waited for once)
+                    uint32_t more = 0;                                           // whether the sums are added to
+                    auto step = [&](uint32_t b_lo, uint32_t a_t) {
 #pragma unroll
-                        for (uint32_t j = 0; j < 4; ++j)
-                            mma_bf16_ts(d_tmem, a_t + 8 * j, mx_desc64(b_lo + 2 * j), idesc, (k > 0 || j > 0) ? 1u : 0u);
+                        for (uint32_t j = 0; j < 4; ++j) { mma_bf16_ts(d_tmem, a_t + 8 * j, mx_desc64(b_lo + 2 * j), idesc, more); more = 1; }
+                    };
+                    auto next_slot = [&]() {
                         if (!p.resident) mma_commit(&bars->slot_empty[slot]);
+                        if (++slot == (uint32_t)p.slots) { slot = 0; slot_ph ^= 1u; }
+                    };
+                    auto next_x = [&]() {
                         mma_commit(&bars->x_empty[s]);
-                        if (++slot == (uint32_t)(p.resident ? nK : p.slots)) { slot = 0; slot_ph ^= 1u; }
                         if (++s == (uint32_t)p.SX) { s = 0; ph ^= 1u; }
+                    };
+                    if (p.x_steps == 2) {
+                        for (int k = 0; k < nK; k += 2) {
+                            if (!mbar_wait(&bars->x_full[s], ph, abort_flag, ws, 0xB310) ||
+                                (wait_w && !mbar_wait(&bars->slot_full[slot], slot_ph, abort_flag, ws, 0xB320))) { ok = false; break; }
+                            tc_fence_after_sync();
+                            const uint32_t b_lo = xb + s * 2u * x16, a_t = tmem_base + p.tmem_scales + slot * kSlotCols;
+                            if (k + 1 < nK) { step(b_lo, a_t); step(b_lo + x16, a_t + 32u); }
+                            else step(b_lo, a_t);
+                            next_slot();
+                            next_x();
+                        }
+                    } else {
+                        for (int k = 0; k < nK; k += 2) {
+                            if ((wait_w && !mbar_wait(&bars->slot_full[slot], slot_ph, abort_flag, ws, 0xB321)) ||
+                                !mbar_wait(&bars->x_full[s], ph, abort_flag, ws, 0xB311)) { ok = false; break; }
+                            tc_fence_after_sync();
+                            const uint32_t a_t = tmem_base + p.tmem_scales + slot * kSlotCols;
+                            step(xb + s * x16, a_t);
+                            next_x();
+                            if (k + 1 < nK) {
+                                if (!mbar_wait(&bars->x_full[s], ph, abort_flag, ws, 0xB312)) { ok = false; break; }
+                                tc_fence_after_sync();
+                                step(xb + s * x16, a_t + 32u);
+                                next_x();
+                            }
+                            next_slot();
+                        }
                     }
                 }
                 if (ok) mma_commit(&bars->epi.acc_full[acc]);
@@ -184,36 +232,48 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
             uint32_t s = 0, lap = 0;
             bool ok = true;
             for (MxWalk w(p.t, blockIdx.x, 0); w.in(p.t) && ok; w.next(p.t)) {
-                for (int k = 0; k < nK; ++k) {
+                for (int k = 0; k < nK; k += p.x_steps) {
                     if (lap >= 1 && !mbar_wait(&bars->x_empty[s], (lap & 1u) ^ 1u, abort_flag, ws, 0xB110)) { ok = false; break; }
-                    mbar_arrive_expect_tx(&bars->x_full[s], p.x_bytes);
-                    tma_load_2d(smem + p.off_x + (size_t)s * p.x_bytes, &tmap_x, &bars->x_full[s], k * 64, w.mt * p.t.N);
+                    uint8_t *st = smem + p.off_x + (size_t)s * p.x_steps * p.x_bytes;
+                    const int n = min(p.x_steps, nK - k);
+                    mbar_arrive_expect_tx(&bars->x_full[s], n * p.x_bytes);
+                    for (int h = 0; h < n; ++h) tma_load_2d(st + h * p.x_bytes, &tmap_x, &bars->x_full[s], (k + h) * 64, w.mt * p.t.N);
                     if (++s == (uint32_t)p.SX) { s = 0; ++lap; }
                 }
             }
         }
     } else if (!kMx && warp < R::kFirstWide + R::kWideWarps) {
-        // ---- widening: group g of four warps takes every second K step, a thread one row of the weights -----------------
+        // ---- widening: a group of four warps takes every second slot (128 columns, two K steps), a thread one row of the weights ------------
         const int group = (warp - R::kFirstWide) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
         bool ok = true;
-        uint32_t s = 0, ph = 0, k0 = 0;                        // k0: K steps before this stage
+        uint32_t s = 0, ph = 0, u0 = 0;                        // u0: slots before this stage
         for (int tile = blockIdx.x; tile < p.t.n_tiles && ok && !(p.resident && tile != (int)blockIdx.x); tile += p.t.grid) {
             for (int step = 0; step < p.nS && ok; ++step) {
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->full[s], ph, abort_flag, ws, 0xB400));
                 if (!ok) break;
                 const uint8_t *st = smem + (size_t)s * p.stage_bytes;
                 const int n = min(4, nK - 4 * step);
-                for (int q = (int)((group ^ k0) & 1u); q < n; q += 2) {
-                    const uint32_t k = k0 + q, slot = p.resident ? k : k % kSlots;
-                    const uint4 a = *reinterpret_cast<const uint4 *>(st + r * 128 + ((2 * q) ^ (r & 7)) * 16);
-                    const uint4 b = *reinterpret_cast<const uint4 *>(st + r * 128 + ((2 * q + 1) ^ (r & 7)) * 16);
-                    const uint32_t codes = *reinterpret_cast<const uint32_t *>(st + kWBytes + (q >> 1) * kMxScaleTile + lane * 16 + quarter * 4) >> (16 * (q & 1));
-                    uint32_t v[32];
-                    mx_widen(v, a, b, codes & 255u, (codes >> 8) & 255u);
-                    if (!p.resident && k >= kSlots) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->slot_empty[slot], ((k / kSlots) & 1u) ^ 1u, abort_flag, ws, 0xB410));
+                for (int t = (int)((group ^ u0) & 1u); 2 * t < n; t += 2) {
+                    const uint32_t u = u0 + t, slot = u % kSlots;               // (weights that stay have at most kSlots)
+                    // scale codes of the tile of 128 columns: four blocks of this row
+                    const uint32_t codes = *reinterpret_cast<const uint32_t *>(st + kWBytes + t * kMxScaleTile + lane * 16 + quarter * 4);
+                    const uint32_t to = tmem_base + ((uint32_t)(quarter * 32) << 16) + p.tmem_scales + slot * kSlotCols;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (2 * t + h >= n) break;
+                        const int q = 2 * t + h;
+                        const uint4 a = *reinterpret_cast<const uint4 *>(st + r * 128 + ((2 * q) ^ (r & 7)) * 16);
+                        const uint4 b = *reinterpret_cast<const uint4 *>(st + r * 128 + ((2 * q + 1) ^ (r & 7)) * 16);
+                        uint32_t v[32];
+                        mx_widen(v, a, b, codes >> (16 * h) & 255u, codes >> (16 * h + 8) & 255u);
+                        if (h == 0) {
+                            if (u >= kSlots) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->slot_empty[slot], ((u / kSlots) & 1u) ^ 1u, abort_flag, ws, 0xB410));
+                            if (!ok) break;
+                            tc_fence_after_sync();
+                        }
+                        tmem_st_x32(to + 32 * h, v);
+                    }
                     if (!ok) break;
-                    tc_fence_after_sync();
-                    tmem_st_x32(tmem_base + ((uint32_t)(quarter * 32) << 16) + p.tmem_scales + slot * 32u, v);
                     tmem_st_wait();
                     tc_fence_before_sync();
                     __syncwarp();
@@ -221,7 +281,7 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bars->empty[s]);
-                k0 += n;
+                u0 += (n + 1) / 2;
                 if (++s == (uint32_t)p.S) { s = 0; ph ^= 1u; }
             }
         }
@@ -268,7 +328,7 @@ bool plan(const npas_mx_linear_desc &d, MxPsParams &p, int sms)
     if (!p.t.n_tiles) return false;
     // Weights that stay: with more than a round of tiles, and few SMs idle for a grid that is a multiple of the tiles across
     const int same = sms / p.t.n_ot * p.t.n_ot, nK = (d.I + 63) / 64;
-    p.resident = !(d.variant >> 16) && p.t.n_tiles > sms && same * 8 >= sms * 7 && (mx ? p.nS <= 4 : nK <= kMaxSlots);
+    p.resident = !(d.variant >> 16) && p.t.n_tiles > sms && same * 8 >= sms * 7 && (mx ? p.nS <= 4 : nK <= 2 * kSlots);
     if (p.resident) mx_tiles_plan(p.t, d, N, kRows, p.t.acc, same);
     p.w_scales = LW.off_scales; p.x_scales = LX.off_scales;
     p.x_bytes = (uint32_t)N * 128u;
@@ -277,25 +337,26 @@ bool plan(const npas_mx_linear_desc &d, MxPsParams &p, int sms)
     p.off_stages = mx && p.resident ? (uint32_t)p.nS * kWStage : 0u;
     p.stage_bytes = p.x_in_stage + (mx ? p.xs_bytes + p.x_bytes : 0u);
     const uint32_t budget = kSmemLimit - (uint32_t)sizeof(MxPsBars) - 128u - 1024u;
-    // Slabs for bf16 outputs with rows on 16-byte boundaries: two where the loads need the room (256 rows of X, no residuals), else four, eight where
+    // Slabs for bf16 outputs with rows on 16-byte boundaries: two where the loads need the room (256 rows of X in 16 bits, or without residuals), else four, eight where
     // residuals are ahead of little else; and the input's ring
-    p.t.NS = !p.y_bf16 || d.O % 8 ? 0 : N == 256 && p.nS > 2 && !d.has_residual ? 2 : mx && d.has_residual && p.nS <= 2 && N == 128 ? 8 : 4;
+    p.t.NS = !p.y_bf16 || d.O % 8 ? 0 : N == 256 && (!mx || (p.nS > 2 && !d.has_residual)) ? 2 : mx && d.has_residual && p.nS <= 2 && N == 128 ? 8 : 4;
     while ((1 << p.t.ns_log) < p.t.NS) ++p.t.ns_log;
-    p.slots = mx ? 0 : p.resident ? nK : kSlots;
-    if (!mx) p.SX = N == 256 ? (p.t.NS == 4 ? 3 : 4) : 6;
-    const uint32_t fixed = p.off_stages + (uint32_t)p.SX * p.x_bytes + (uint32_t)p.t.NS * kMxSlabBytes;
+    p.slots = mx ? 0 : p.resident ? (nK + 1) / 2 : kSlots;
+    p.x_steps = N == 256 ? 1 : 2;
+    if (!mx) p.SX = N == 256 ? 4 : 3;
+    const uint32_t fixed = p.off_stages + (uint32_t)(p.SX * p.x_steps) * p.x_bytes + (uint32_t)p.t.NS * kMxSlabBytes;
     if (fixed >= budget) return false;
     p.S = (int)((budget - fixed) / p.stage_bytes);
     if (p.S > kMaxStages) p.S = kMaxStages;
     if (p.S < 2) return false;
     p.off_x = p.off_stages + (uint32_t)p.S * p.stage_bytes;
-    p.t.off_slabs = p.off_x + (uint32_t)p.SX * p.x_bytes;
+    p.t.off_slabs = p.off_x + (uint32_t)(p.SX * p.x_steps) * p.x_bytes;
     p.off_bar = round_up(p.t.off_slabs + (uint32_t)p.t.NS * kMxSlabBytes, 128);
     p.smem_bytes = p.off_bar + (uint32_t)sizeof(MxPsBars) + 1024u;
     if (p.smem_bytes > kSmemLimit) return false;
     p.tmem_scales = 256;
     p.scale_cols = (p.resident ? 0 : 8) + 2 * (uint32_t)N / 32;
-    const uint32_t cols = p.tmem_scales + (mx ? (p.resident ? 8u * p.nS : 0u) + p.scale_cols * p.S : 32u * p.slots);
+    const uint32_t cols = p.tmem_scales + (mx ? (p.resident ? 8u * p.nS : 0u) + p.scale_cols * p.S : kSlotCols * p.slots);
     p.tmem_cols = 32;
     while (p.tmem_cols < cols) p.tmem_cols *= 2;
     return p.tmem_cols <= 512;

@@ -10,7 +10,7 @@
 //   16-bit input to be quantised: the eight warps that have nothing to do before the epilogue quantise the CTA's share of X into the stage, a row
 //     of 256 columns a warp, instead of a launch of its own ahead of this one (a call of one row 6.0 -> FIXME us of host time).
 //   16-bit input: eight warps widen the weights, a thread a row: 32 bytes -> 64 bf16 values in 32 columns of tensor memory, from where the
-//     MMAs of kind::f16 take their first operand.  Four such slots; weights and inputs have rings of their own (256 and 64 columns a
+//     MMAs of kind::f16 take their first operand.  Slots of two steps; weights and inputs have rings of their own (256 and 128 columns a
 //     stage).  Widening costs 2.4 instructions a weight, at the issue rate about what HBM delivers.
 // Every wait is bounded.
 #include "mx_tc.cuh"
@@ -27,14 +27,15 @@ constexpr int kXWarp = 2 + kEpiWarps;                      // copies of a 16-bit
 constexpr int kThreads = (kXWarp + 1) * 32;                // warp 0: copies, warp 1: MMAs
 constexpr int kRows = 128;
 constexpr int kStepCols = 256;                             // columns of a weight stage
-constexpr int kMaxStages = 6, kMaxXStages = 8, kSlots = 4;
+constexpr int kMaxStages = 6, kMaxXStages = 4, kSlots = 4;
+constexpr uint32_t kSlotCols = 64;                         // tensor memory of a slot: 128 widened columns of the weights
 constexpr int kMaxSplit = 8;                               // portable cluster size
 constexpr uint32_t kSmemLimit = 232448, kSmemHalf = 115712;   // of a CTA alone on its SM, of one of two (1 KB each is the system's)
 constexpr uint32_t kWBytes = kRows * 128;
 constexpr uint32_t kScaleBytes = 2 * kMxScaleTile;         // of 128 rows and a stage
 
 struct MxSwParams {
-    int M, I, O, N, KS, nS, spr, nMT, nOT, nKT, S, SX, cpr;   // spr: steps per CTA; SX: stages of the input (16 bits); cpr: input rows a CTA owns
+    int M, I, O, N, KS, nS, spr, nMT, nOT, nKT, S, SX, slots, cpr;   // spr: steps per CTA; SX: stages of two K steps of the input (16 bits); cpr: input rows a CTA owns
     int relu, y_bf16;
     uint32_t x_bytes, stage_bytes, off_x, off_red, red_pitch, off_bar, smem_bytes, tmem_cols, tmem_scales;
     uint64_t w_scales, x_scales;                           // offsets of the scales in the blobs
@@ -93,7 +94,7 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
     if (tid == 0) {
         for (int s = 0; s < p.S; ++s) { mbar_init(&bars->full[s], kIn == kQuantize ? 1 + kEpiWarps : 1); mbar_init(&bars->empty[s], kMx ? 1 : kEpiWarps); }
         for (int s = 0; s < p.SX; ++s) { mbar_init(&bars->x_full[s], 1); mbar_init(&bars->x_empty[s], 1); }
-        for (int s = 0; s < kSlots; ++s) { mbar_init(&bars->slot_full[s], kEpiWarps / 2); mbar_init(&bars->slot_empty[s], 1); }
+        for (int s = 0; s < p.slots; ++s) { mbar_init(&bars->slot_full[s], kEpiWarps / 2); mbar_init(&bars->slot_empty[s], 1); }
         mbar_init(&bars->acc_full, 1);
         bars->abort_flag = 0;
         fence_barrier_init();
@@ -157,19 +158,23 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
                     if (++s == (uint32_t)p.S) { s = 0; ph ^= 1u; }
                 }
             } else {
-                uint32_t sx = 0, phx = 0;
-                const uint32_t idesc = idesc_bf16_f32(128, (uint32_t)p.N), xb = base + p.off_x;
-                for (int k = 0; k < k_n; ++k) {
-                    const uint32_t slot = k % kSlots;
-                    if (!mbar_wait(&bars->x_full[sx], phx, abort_flag, ws, 0xA310) ||
-                        !mbar_wait(&bars->slot_full[slot], (k / kSlots) & 1u, abort_flag, ws, 0xA320)) { go = false; break; }
-                    tc_fence_after_sync();
-                    const uint32_t b_lo = ((xb + sx * p.x_bytes) >> 4) | kMxDescLboOne, a_t = tmem_base + p.tmem_scales + slot * 32u;
+                // a slot and a stage of X are two K steps: eight MMAs without a branch between them
+                uint32_t sx = 0, phx = 0, slot = 0, slot_ph = 0, more = 0;
+                const uint32_t idesc = idesc_bf16_f32(128, (uint32_t)p.N), x16 = p.x_bytes >> 4, xb = ((base + p.off_x) >> 4) | kMxDescLboOne;
+                auto step = [&](uint32_t b_lo, uint32_t a_t) {
 #pragma unroll
-                    for (uint32_t j = 0; j < 4; ++j)
-                        mma_bf16_ts(tmem_base, a_t + 8 * j, mx_desc64(b_lo + 2 * j), idesc, (k > 0 || j > 0) ? 1u : 0u);
+                    for (uint32_t j = 0; j < 4; ++j) { mma_bf16_ts(tmem_base, a_t + 8 * j, mx_desc64(b_lo + 2 * j), idesc, more); more = 1; }
+                };
+                for (int k = 0; k < k_n; k += 2) {
+                    if (!mbar_wait(&bars->x_full[sx], phx, abort_flag, ws, 0xA310) ||
+                        !mbar_wait(&bars->slot_full[slot], slot_ph, abort_flag, ws, 0xA320)) { go = false; break; }
+                    tc_fence_after_sync();
+                    const uint32_t b_lo = xb + sx * 2u * x16, a_t = tmem_base + p.tmem_scales + slot * kSlotCols;
+                    if (k + 1 < k_n) { step(b_lo, a_t); step(b_lo + x16, a_t + 32u); }
+                    else step(b_lo, a_t);
                     mma_commit(&bars->slot_empty[slot]);
                     mma_commit(&bars->x_empty[sx]);
+                    if (++slot == (uint32_t)p.slots) { slot = 0; slot_ph ^= 1u; }
                     if (++sx == (uint32_t)p.SX) { sx = 0; phx ^= 1u; }
                 }
             }
@@ -179,10 +184,12 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
     } else if (warp == kXWarp) {
         if (!kMx && lane == 0) {
             uint32_t sx = 0, lap = 0;
-            for (int k = 0; k < k_n; ++k) {
+            for (int k = 0; k < k_n; k += 2) {
                 if (lap >= 1 && !mbar_wait(&bars->x_empty[sx], (lap & 1u) ^ 1u, abort_flag, ws, 0xA110)) break;
-                mbar_arrive_expect_tx(&bars->x_full[sx], p.x_bytes);
-                tma_load_2d(smem + p.off_x + (size_t)sx * p.x_bytes, &tmap_x, &bars->x_full[sx], (4 * s_lo + k) * 64, mt * p.N);
+                uint8_t *st = smem + p.off_x + (size_t)sx * 2 * p.x_bytes;
+                const int n = min(2, k_n - k);
+                mbar_arrive_expect_tx(&bars->x_full[sx], n * p.x_bytes);
+                for (int h = 0; h < n; ++h) tma_load_2d(st + h * p.x_bytes, &tmap_x, &bars->x_full[sx], (4 * s_lo + k + h) * 64, mt * p.N);
                 if (++sx == (uint32_t)p.SX) { sx = 0; ++lap; }
             }
         }
@@ -217,7 +224,7 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
             if (++s == (uint32_t)p.S) { s = 0; ++lap; }
         }
     } else if (kIn == kWide) {
-        // ---- widening: group g of four warps takes every second K step, a thread one row of the weights -----------------
+        // ---- widening: a group of four warps takes every second slot (128 columns, two K steps), a thread one row of the weights ------------
         const int group = (warp - 2) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
         bool ok = true;
         uint32_t s = 0, ph = 0;
@@ -225,18 +232,27 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->full[s], ph, abort_flag, ws, 0xA400));
             if (!ok) break;
             const uint8_t *st = smem + (size_t)s * p.stage_bytes;
-            for (int q = group; q < 4 && 4 * i + q < k_n; q += 2) {
-                const int k = 4 * i + q;
-                const uint32_t slot = k % kSlots;
-                const uint4 a = *reinterpret_cast<const uint4 *>(st + r * 128 + ((2 * q) ^ (r & 7)) * 16);
-                const uint4 b = *reinterpret_cast<const uint4 *>(st + r * 128 + ((2 * q + 1) ^ (r & 7)) * 16);
-                const uint32_t codes = *reinterpret_cast<const uint32_t *>(st + kWBytes + (q >> 1) * kMxScaleTile + lane * 16 + quarter * 4) >> (16 * (q & 1));
-                uint32_t v[32];
-                mx_widen(v, a, b, codes & 255u, (codes >> 8) & 255u);
-                if (k >= kSlots) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->slot_empty[slot], ((k / kSlots) & 1u) ^ 1u, abort_flag, ws, 0xA410));
+            const int u = 2 * i + group, n = min(2, k_n - 2 * u);               // this group's slot of the stage, K steps in it
+            if (n > 0) {
+                const uint32_t lap = (uint32_t)u / (uint32_t)p.slots, slot = (uint32_t)u - lap * (uint32_t)p.slots;
+                const uint32_t codes = *reinterpret_cast<const uint32_t *>(st + kWBytes + group * kMxScaleTile + lane * 16 + quarter * 4);
+                const uint32_t to = tmem_base + ((uint32_t)(quarter * 32) << 16) + p.tmem_scales + slot * kSlotCols;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (h >= n) break;
+                    const int q = 2 * group + h;
+                    const uint4 a = *reinterpret_cast<const uint4 *>(st + r * 128 + ((2 * q) ^ (r & 7)) * 16);
+                    const uint4 b = *reinterpret_cast<const uint4 *>(st + r * 128 + ((2 * q + 1) ^ (r & 7)) * 16);
+                    uint32_t v[32];
+                    mx_widen(v, a, b, codes >> (16 * h) & 255u, codes >> (16 * h + 8) & 255u);
+                    if (h == 0) {
+                        if (lap) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->slot_empty[slot], (lap & 1u) ^ 1u, abort_flag, ws, 0xA410));
+                        if (!ok) break;
+                        tc_fence_after_sync();
+                    }
+                    tmem_st_x32(to + 32 * h, v);
+                }
                 if (!ok) break;
-                tc_fence_after_sync();
-                tmem_st_x32(tmem_base + ((uint32_t)(quarter * 32) << 16) + p.tmem_scales + slot * 32u, v);
                 tmem_st_wait();
                 tc_fence_before_sync();
                 __syncwarp();
@@ -338,23 +354,24 @@ bool shape(MxSwParams &p, bool mx, int ks, int sms)
     const uint32_t budget = limit - fixed;
     p.SX = 0;
     if (!mx) {
-        // the input's ring (of 64 columns a stage)
+        // the input's ring (of 128 columns a stage)
         p.SX = kMaxXStages;
-        while (p.SX > 2 && (uint32_t)p.SX * p.x_bytes + 3 * p.stage_bytes > budget) --p.SX;
-        if ((uint32_t)p.SX * p.x_bytes >= budget) return false;
+        while (p.SX > 1 && (uint32_t)p.SX * 2 * p.x_bytes + 3 * p.stage_bytes > budget) --p.SX;
+        if ((uint32_t)p.SX * 2 * p.x_bytes >= budget) return false;
     }
-    p.S = (int)((budget - (uint32_t)p.SX * p.x_bytes) / p.stage_bytes);
+    p.S = (int)((budget - (uint32_t)p.SX * 2 * p.x_bytes) / p.stage_bytes);
     if (p.S > kMaxStages) p.S = kMaxStages;
     if (p.S > p.spr) p.S = p.spr;
     if (p.S < 1 || (p.S < 2 && p.spr > 1)) return false;
     p.off_x = (uint32_t)p.S * p.stage_bytes;
-    p.off_red = p.off_x + (uint32_t)p.SX * p.x_bytes;
+    p.off_red = p.off_x + (uint32_t)p.SX * 2 * p.x_bytes;
     p.off_bar = round_up(p.off_red + red, 128);
     p.smem_bytes = p.off_bar + (uint32_t)sizeof(MxSwBars) + 1024u;
     if (p.smem_bytes > kSmemLimit) return false;
     // columns of tensor memory: the sums, then scales of every stage (4-bit) or the widened weights
     p.tmem_scales = round_up((uint32_t)p.N, 32);
-    const uint32_t cols = p.tmem_scales + (mx ? 16u * p.S : 32u * kSlots);
+    p.slots = limit == kSmemHalf ? 2 : kSlots;
+    const uint32_t cols = p.tmem_scales + (mx ? 16u * p.S : kSlotCols * p.slots);
     p.tmem_cols = 32;
     while (p.tmem_cols < cols) p.tmem_cols *= 2;
     return p.tmem_cols <= 512;
