@@ -9,7 +9,7 @@
 //     step (a set of columns per ring stage, so that no copy meets an MMA that still reads), MMAs of kind::mxf4 over 64 columns.
 //   16-bit input to be quantised: the eight warps that have nothing to do before the epilogue quantise the CTA's share of X into the stage, a row
 //     of 256 columns a warp, instead of a launch of its own ahead of this one (a call of one row 6.0 -> FIXME us of host time).
-//   16-bit input: eight warps widen the weights, a thread a row: 32 bytes -> 64 bf16 values in 32 columns of tensor memory, from where the
+//   16-bit input: sixteen warps widen the weights, a thread a row: 32 bytes -> 64 bf16 values in 32 columns of tensor memory, from where the
 //     MMAs of kind::f16 take their first operand.  Slots of two steps; weights and inputs have rings of their own (256 and 128 columns a
 //     stage).  Widening costs 2.4 instructions a weight, at the issue rate about what HBM delivers.
 // Every wait is bounded.
@@ -22,9 +22,6 @@ using namespace tc;
 
 namespace {
 
-constexpr int kEpiWarps = 8;                               // widening, then the epilogue
-constexpr int kXWarp = 2 + kEpiWarps;                      // copies of a 16-bit input
-constexpr int kThreads = (kXWarp + 1) * 32;                // warp 0: copies, warp 1: MMAs
 constexpr int kRows = 128;
 constexpr int kStepCols = 256;                             // columns of a weight stage
 constexpr int kMaxStages = 6, kMaxXStages = 4, kSlots = 4;
@@ -72,12 +69,19 @@ template <bool kBf16> __device__ __forceinline__ void store_y(void *y, int64_t a
 // what the input is: a blob, 16 bits to be quantised, 16 bits
 enum MxIn { kBlob, kQuantize, kWide };
 
+// warps: 0 copies, 1 MMAs, then those that widen or quantise and make the epilogue, last the copies of a 16-bit input.  Sixteen widen: eight
+// took 500 cycles for two K steps each, the MMAs of a step 50 to 250
+template <MxIn kIn> struct SwRoles {
+    static constexpr int kEpiWarps = kIn == kWide ? 16 : 8, kXWarp = 2 + kEpiWarps, kThreads = (kXWarp + 1) * 32, kPerSm = kIn == kWide ? 1 : 2;
+};
+
 template <MxIn kIn, bool kBf16>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(SwRoles<kIn>::kThreads, SwRoles<kIn>::kPerSm)
 linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w, const MxSwParams p, const uint8_t *xin,
                     const uint8_t *wblob, const float *bias, const void *res, void *y, uint32_t *ws)
 {
     constexpr bool kMx = kIn != kWide;
+    constexpr int kEpiWarps = SwRoles<kIn>::kEpiWarps, kXWarp = SwRoles<kIn>::kXWarp, kThreads = SwRoles<kIn>::kThreads;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     MxSwBars *bars = reinterpret_cast<MxSwBars *>(smem + p.off_bar);
@@ -94,7 +98,7 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
     if (tid == 0) {
         for (int s = 0; s < p.S; ++s) { mbar_init(&bars->full[s], kIn == kQuantize ? 1 + kEpiWarps : 1); mbar_init(&bars->empty[s], kMx ? 1 : kEpiWarps); }
         for (int s = 0; s < p.SX; ++s) { mbar_init(&bars->x_full[s], 1); mbar_init(&bars->x_empty[s], 1); }
-        for (int s = 0; s < p.slots; ++s) { mbar_init(&bars->slot_full[s], kEpiWarps / 2); mbar_init(&bars->slot_empty[s], 1); }
+        for (int s = 0; s < p.slots; ++s) { mbar_init(&bars->slot_full[s], 4); mbar_init(&bars->slot_empty[s], 1); }
         mbar_init(&bars->acc_full, 1);
         bars->abort_flag = 0;
         fence_barrier_init();
@@ -224,23 +228,23 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
             if (++s == (uint32_t)p.S) { s = 0; ++lap; }
         }
     } else if (kIn == kWide) {
-        // ---- widening: a group of four warps takes every second slot (128 columns, two K steps), a thread one row of the weights ------------
-        const int group = (warp - 2) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+        // ---- widening: a group of four warps takes every fourth slot (128 columns, two K steps), a thread one row of the weights ------------
+        const int group = (warp - 2) >> 2, quarter = warp & 3, r = quarter * 32 + lane, t = group & 1;       // t: which slot of a stage
         bool ok = true;
         uint32_t s = 0, ph = 0;
         for (int i = 0; i < s_n && ok; ++i) {
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bars->full[s], ph, abort_flag, ws, 0xA400));
             if (!ok) break;
             const uint8_t *st = smem + (size_t)s * p.stage_bytes;
-            const int u = 2 * i + group, n = min(2, k_n - 2 * u);               // this group's slot of the stage, K steps in it
+            const int u = 2 * i + t, n = (i & 1) == (group >> 1) ? min(2, k_n - 2 * u) : 0;    // this group's slot of the stage, K steps in it
             if (n > 0) {
                 const uint32_t lap = (uint32_t)u / (uint32_t)p.slots, slot = (uint32_t)u - lap * (uint32_t)p.slots;
-                const uint32_t codes = *reinterpret_cast<const uint32_t *>(st + kWBytes + group * kMxScaleTile + lane * 16 + quarter * 4);
+                const uint32_t codes = *reinterpret_cast<const uint32_t *>(st + kWBytes + t * kMxScaleTile + lane * 16 + quarter * 4);
                 const uint32_t to = tmem_base + ((uint32_t)(quarter * 32) << 16) + p.tmem_scales + slot * kSlotCols;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     if (h >= n) break;
-                    const int q = 2 * group + h;
+                    const int q = 2 * t + h;
                     const uint4 a = *reinterpret_cast<const uint4 *>(st + r * 128 + ((2 * q) ^ (r & 7)) * 16);
                     const uint4 b = *reinterpret_cast<const uint4 *>(st + r * 128 + ((2 * q + 1) ^ (r & 7)) * 16);
                     uint32_t v[32];
@@ -348,8 +352,8 @@ bool shape(MxSwParams &p, bool mx, int ks, int sms)
     const uint32_t fixed = red + (uint32_t)sizeof(MxSwBars) + 128u + 1024u;
     p.x_bytes = (uint32_t)p.N * 128u;
     p.stage_bytes = round_up(kWBytes + (mx ? 2 * kScaleBytes + p.x_bytes : kScaleBytes), 1024);
-    // (two CTAs on an SM where there are more CTAs than SMs)
-    const uint32_t limit = (long long)p.nMT * p.nOT * ks > sms ? kSmemHalf : kSmemLimit;
+    // (two CTAs on an SM where there are more CTAs than SMs; those that widen have too many warps for that)
+    const uint32_t limit = mx && (long long)p.nMT * p.nOT * ks > sms ? kSmemHalf : kSmemLimit;
     if (fixed >= limit) return false;
     const uint32_t budget = limit - fixed;
     p.SX = 0;
@@ -370,7 +374,7 @@ bool shape(MxSwParams &p, bool mx, int ks, int sms)
     if (p.smem_bytes > kSmemLimit) return false;
     // columns of tensor memory: the sums, then scales of every stage (4-bit) or the widened weights
     p.tmem_scales = round_up((uint32_t)p.N, 32);
-    p.slots = limit == kSmemHalf ? 2 : kSlots;
+    p.slots = kSlots;
     const uint32_t cols = p.tmem_scales + (mx ? 16u * p.S : kSlotCols * p.slots);
     p.tmem_cols = 32;
     while (p.tmem_cols < cols) p.tmem_cols *= 2;
@@ -427,7 +431,7 @@ npas_status linear_mx_sw_launch(const npas_mx_linear_desc &d, const void *x, int
                       : d.quantize_x ? (p.y_bf16 ? linear_mx_sw_kernel<kQuantize, true> : linear_mx_sw_kernel<kQuantize, false>)
                                      : (p.y_bf16 ? linear_mx_sw_kernel<kWide, true> : linear_mx_sw_kernel<kWide, false>);
     if (allow_dynamic_smem(reinterpret_cast<const void *>(kernel), (int)kSmemLimit) != NPAS_OK) return NPAS_ERR_CUDA;
-    const dim3 grid((unsigned)(p.nMT * p.nOT * p.KS)), block(kThreads);
+    const dim3 grid((unsigned)(p.nMT * p.nOT * p.KS)), block(blob || d.quantize_x ? SwRoles<kBlob>::kThreads : SwRoles<kWide>::kThreads);
     const uint8_t *xb = static_cast<const uint8_t *>(x), *wb = static_cast<const uint8_t *>(w);
     const cudaError_t e = p.KS > 1 ? launch_pdl_cluster(Launch(), kernel, grid, block, p.KS, p.smem_bytes, st, tmx, tmw, p, xb, wb, bias, res, y, ws)
                                    : launch_pdl(Launch(), kernel, grid, block, p.smem_bytes, st, tmx, tmw, p, xb, wb, bias, res, y, ws);
