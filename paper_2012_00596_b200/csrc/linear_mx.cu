@@ -1,7 +1,6 @@
 // Entry points of the GEMM with microscaled 4-bit weights: argument checks, workspace, the choice of a kernel.
 #include "internal_api.h"
-#include "mx.cuh"
-#include "tc_common.cuh"
+#include "mx_tc.cuh"
 
 namespace npas {
 
@@ -123,27 +122,38 @@ size_t scratch_bytes(const npas_mx_linear_desc &d)
 
 constexpr int kPitchThreads = 256;
 
-// A thread writes 16 bytes of a row; columns past the end are zeros.
-__global__ void __launch_bounds__(kPitchThreads) mx_pitch_kernel(int64_t M, int I, int64_t pieces, const uint16_t *x, uint4 *out)
+// `lanes` neighbouring threads have a row and write 16 bytes each at a time, four on their way together; columns past the end are zeros.
+__global__ void __launch_bounds__(kPitchThreads) mx_pitch_kernel(int64_t M, int I, int pieces, int lanes, const uint16_t *x, uint4 *out)
 {
     tc::pdl_trigger();
     tc::pdl_wait();
     x = tc::behind_wait(x);
-    for (int64_t i = (int64_t)blockIdx.x * kPitchThreads + threadIdx.x; i < M * pieces; i += (int64_t)gridDim.x * kPitchThreads) {
-        const int64_t row = i / pieces;
-        const int c = (int)(i - row * pieces) * 8;
-        uint32_t v[8];
+    constexpr int kAhead = 4;
+    const int rows = kPitchThreads / lanes, lane = threadIdx.x % lanes;
+    for (int64_t row = (int64_t)blockIdx.x * rows + threadIdx.x / lanes; row < M; row += (int64_t)gridDim.x * rows)
+        for (int p0 = lane; p0 < pieces; p0 += kAhead * lanes) {
+            tc::MxRaw<4> raw[kAhead];
+            const uint16_t *from = x + row * I + 8 * p0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = c + j < I ? x[row * I + c + j] : 0u;
-        out[i] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
-    }
+            for (int k = 0; k < kAhead; ++k) tc::mx_load_raw(raw[k], from + 8 * k * lanes, min(I - 8 * (p0 + k * lanes), 8), x + M * I);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int p = p0 + k * lanes;
+                uint32_t v[4];
+                tc::mx_align(v, raw[k], from + 8 * k * lanes, min(I - 8 * p, 8));
+                if (p < pieces) out[row * pieces + p] = make_uint4(v[0], v[1], v[2], v[3]);
+            }
+        }
 }
 
 npas_status pitch_launch(const npas_mx_linear_desc &d, const void *x, void *out, cudaStream_t st)
 {
-    const int64_t pieces = pitch_of(d) / 8, blocks = (d.M * pieces + kPitchThreads - 1) / kPitchThreads, most = (int64_t)sm_count() * 16;
+    const int pieces = (int)(pitch_of(d) / 8);
+    int lanes = 1;
+    while (lanes < 32 && lanes < pieces) lanes *= 2;
+    const int64_t rows = kPitchThreads / lanes, blocks = ((int64_t)d.M + rows - 1) / rows, most = (int64_t)sm_count() * 32;
     const cudaError_t e = tc::launch_pdl(Launch(), mx_pitch_kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(kPitchThreads), 0, st, (int64_t)d.M,
-                                         (int)d.I, pieces, static_cast<const uint16_t *>(x), static_cast<uint4 *>(out));
+                                         (int)d.I, pieces, lanes, static_cast<const uint16_t *>(x), static_cast<uint4 *>(out));
     count_launch();
     return e == cudaSuccess ? launch_status() : NPAS_ERR_CUDA;
 }

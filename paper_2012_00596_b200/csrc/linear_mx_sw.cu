@@ -211,7 +211,14 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
             const int c = (s_lo + i) * kStepCols + lane * 8;
             for (int r = warp - 2; r < rows; r += kEpiWarps) {
                 uint32_t v[4];
-                mx_load8(v, x + (int64_t)(mt * p.N + r) * p.I, c, p.I, whole);
+                const uint16_t *from = x + (int64_t)(mt * p.N + r) * p.I + c;
+                const int n = max(0, min(p.I - c, 8));
+                if (whole) mx_load_whole(v, from, n > 0);
+                else {
+                    MxRaw<4> raw;
+                    mx_load_raw(raw, from, n, x + (int64_t)p.M * p.I);
+                    mx_align(v, raw, from, n);
+                }
                 uint32_t top = mx_top8(v);
                 top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
                 top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));

@@ -11,6 +11,8 @@
 // is put together in shared memory and leaves in whole sectors.  Maxima and scaling on pairs of bf16: with every element as a float
 // 125 instructions for eight of them bound it (200704x256 57 us, now 21: 94 % of the copy rate; fp32 36.7, 97 %; back 22.3 and
 // 38.6).
+#include <type_traits>
+
 #include "mx_tc.cuh"
 
 namespace npas {
@@ -19,12 +21,13 @@ namespace {
 
 constexpr int kThreads = 256;
 
-template <typename T, bool kParts, int kLanes>
-__global__ void __launch_bounds__(kThreads) quantize_mx_kernel(int rows, int cols, int whole, int n_parts, const T *src, uint8_t *blob)
+// kWhole: mx_load_whole can be used; else a block has half a tile at most (its loads take more registers)
+template <typename T, bool kParts, int kLanes, bool kWhole>
+__global__ void __launch_bounds__(kThreads) quantize_mx_kernel(int rows, int cols, int n_parts, const T *src, uint8_t *blob)
 {
     __shared__ __align__(16) uint8_t scales[kMxScaleTile];
     const MxLayout L = mx_layout(rows, cols);
-    constexpr int kRowsPerPass = kThreads / kLanes, kPasses = kMxTileRows / kRowsPerPass;
+    constexpr int kRowsPerPass = kThreads / kLanes, kTilePasses = kMxTileRows / kRowsPerPass, kPasses = kWhole ? kTilePasses : 4;
     const int parts = kParts ? n_parts : 1;
     const uint32_t tile = blockIdx.x / parts, part = blockIdx.x - tile * parts, rt = tile / L.nKT, kt = tile - rt * L.nKT;
     const int rows_part = kMxTileRows / parts, row_lo = (int)part * rows_part;   // this block's rows of the tile
@@ -37,19 +40,21 @@ __global__ void __launch_bounds__(kThreads) quantize_mx_kernel(int rows, int col
     uint8_t *values = blob + L.off_values;
     // passes that have rows (a tile of few rows is latency: one row of 2048 columns took 2.2 us with all eight)
     const int passes = (max(rows_here, 0) + kRowsPerPass - 1) / kRowsPerPass;
-    if (kLanes < 16 || passes < kPasses) {
+    if (kLanes < 16 || passes < kTilePasses) {
         if (threadIdx.x < kMxTileRows) reinterpret_cast<uint32_t *>(scales)[threadIdx.x] = 0u;
         __syncthreads();
     }
     constexpr int W = sizeof(T) == 2 ? 4 : 8;
-    uint32_t v[kPasses][W];
+    typename std::conditional<kWhole, uint32_t[W], tc::MxRaw<W>>::type raw[kPasses];
     const int64_t row0 = (int64_t)rt * kMxTileRows + r0;
-    const T *from = src + row0 * cols;
+    const T *from = src + row0 * cols + c, *end = src + (int64_t)rows * cols;
+    const int n = max(0, min(cols - c, 8));
 #pragma unroll
     for (int p = 0; p < kPasses; ++p) {
         if (p >= passes) break;
-        tc::mx_load8(v[p], from, p * kRowsPerPass < left ? c : cols, cols, whole);
-        from += (int64_t)kRowsPerPass * cols;
+        const bool there = p * kRowsPerPass < left && n > 0;
+        if constexpr (kWhole) tc::mx_load_whole(raw[p], from + (int64_t)p * kRowsPerPass * cols, there);
+        else tc::mx_load_raw(raw[p], from + (int64_t)p * kRowsPerPass * cols, there ? n : 0, end);
     }
     uint8_t *to = values + (uint64_t)row0 * L.pitch + c / 2;
     const bool stored = (uint32_t)c < 2 * L.pitch;
@@ -57,12 +62,19 @@ __global__ void __launch_bounds__(kThreads) quantize_mx_kernel(int rows, int col
     for (int p = 0; p < kPasses; ++p) {
         if (p >= passes) break;
         const int r = p * kRowsPerPass + r0;
-        uint32_t top = tc::mx_top8(v[p]);
+        uint32_t v[W];
+        if constexpr (kWhole) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) v[i] = raw[p][i];
+        } else {
+            tc::mx_align(v, raw[p], from + (int64_t)p * kRowsPerPass * cols, p * kRowsPerPass < left ? n : 0);
+        }
+        uint32_t top = tc::mx_top8(v);
         top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
         top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
         const uint32_t code = tc::mx_code(top);
         float f[8];
-        tc::mx_scaled8(f, v[p], code);
+        tc::mx_scaled8(f, v, code);
         const uint32_t word = tc::mx_cvt_e2m1x8(f);
         if (p * kRowsPerPass < left && stored) *reinterpret_cast<uint32_t *>(to) = code == 255 ? 0u : word;
         to += (uint64_t)kRowsPerPass * L.pitch;
@@ -171,12 +183,12 @@ __global__ void __launch_bounds__(kThreads) dequantize_mx_kernel(int rows, int c
 // The launch of either kernel.  Up to 64 columns: eight lanes a row instead of sixteen (the rest of the tile is not there).  Small matrices: a
 // tile in parts of 64, 32 or 16 rows, so that more SMs have work and a thread has fewer passes.
 struct Shape { int narrow, parts, whole; dim3 grid; };
-Shape shape_of(const npas_mx_desc &d, const MxLayout &L)
+Shape shape_of(const npas_mx_desc &d, const MxLayout &L, bool quantize)
 {
     Shape s;
     s.narrow = d.cols <= 64;
     s.whole = d.cols % 8 == 0;
-    s.parts = 1;
+    s.parts = !quantize || s.whole || s.narrow ? 1 : 2;
     const uint64_t tiles = (uint64_t)L.nRT * L.nKT;
     while (s.parts < (s.narrow ? 4 : 8) && tiles * s.parts * 2 <= 6ull * sm_count()) s.parts *= 2;
     s.grid = dim3((unsigned)(tiles * s.parts));
@@ -185,9 +197,10 @@ Shape shape_of(const npas_mx_desc &d, const MxLayout &L)
 template <typename T>
 cudaError_t quantize_any(const npas_mx_desc &d, const Shape &s, const void *src, void *blob, cudaStream_t st, Launch how)
 {
-    const auto kernel = s.narrow ? (s.parts > 1 ? quantize_mx_kernel<T, true, 8> : quantize_mx_kernel<T, false, 8>)
-                                 : (s.parts > 1 ? quantize_mx_kernel<T, true, 16> : quantize_mx_kernel<T, false, 16>);
-    return tc::launch_pdl(how, kernel, s.grid, dim3(kThreads), 0, st, (int)d.rows, (int)d.cols, s.whole, s.parts, static_cast<const T *>(src),
+    const auto kernel = !s.whole ? (s.narrow ? quantize_mx_kernel<T, true, 8, false> : quantize_mx_kernel<T, true, 16, false>)
+                      : s.narrow ? (s.parts > 1 ? quantize_mx_kernel<T, true, 8, true> : quantize_mx_kernel<T, false, 8, true>)
+                                 : (s.parts > 1 ? quantize_mx_kernel<T, true, 16, true> : quantize_mx_kernel<T, false, 16, true>);
+    return tc::launch_pdl(how, kernel, s.grid, dim3(kThreads), 0, st, (int)d.rows, (int)d.cols, s.parts, static_cast<const T *>(src),
                           static_cast<uint8_t *>(blob));
 }
 template <typename T>
@@ -203,7 +216,7 @@ cudaError_t dequantize_any(const npas_mx_desc &d, const Shape &s, const void *bl
 
 npas_status quantize_mx_launch(const npas_mx_desc &d, const void *src, void *blob, cudaStream_t st, Launch how)
 {
-    const Shape s = shape_of(d, mx_layout(d.rows, d.cols));
+    const Shape s = shape_of(d, mx_layout(d.rows, d.cols), true);
     const cudaError_t e = d.src_dtype == NPAS_BF16 ? quantize_any<uint16_t>(d, s, src, blob, st, how) : quantize_any<float>(d, s, src, blob, st, how);
     count_launch();
     return e == cudaSuccess ? launch_status() : NPAS_ERR_CUDA;
@@ -245,7 +258,7 @@ npas_status npas_dequantize_mx(const npas_mx_desc *d, const void *blob, size_t b
     const MxLayout L = mx_layout(d->rows, d->cols);
     if (blob_bytes < L.total) return NPAS_ERR_BUFFER_TOO_SMALL;
     if (blob == out) return NPAS_ERR_UNSUPPORTED;
-    const Shape f = shape_of(*d, L);
+    const Shape f = shape_of(*d, L, false);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const cudaError_t e = out_dtype == NPAS_BF16 ? dequantize_any<uint16_t>(*d, f, blob, out, st) : dequantize_any<float>(*d, f, blob, out, st);
     count_launch();

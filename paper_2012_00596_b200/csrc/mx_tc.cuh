@@ -170,30 +170,75 @@ __device__ __forceinline__ uint32_t mx_cvt_e2m1x8(const float (&v)[8])
     return d;
 }
 
-// Eight columns of a row as they are, zeros past the end (bf16 in pairs: four words; fp32: eight).  `whole`: rows start on 16-byte
-// boundaries and 8 divides the columns.
+// Eight columns of a row as they are, zeros past the end: bf16 in pairs (four words), fp32 (eight).  `whole`: rows start on 16-byte
+// boundaries and 8 divides the columns; else in two halves, the loads and what waits for them: the aligned 16-byte pieces that hold a column
+// of them (never one past `end`, where the matrix ends), then the words moved to their places.
+template <int W> struct MxRaw {
+    uint32_t w[W == 4 ? 8 : 12];
+};
 template <int W>
-__device__ __forceinline__ void mx_load8(uint32_t (&v)[W], const void *row, int c, int cols, bool whole)
+__device__ __forceinline__ void mx_load_whole(uint32_t (&v)[W], const void *at, bool there)
 {
-    constexpr bool kHalf = W == 4;
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] = 0u;
-    if (whole) {
-        if (c >= cols) return;
-        if constexpr (kHalf) {
-            const uint4 u = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(row) + c);
-            v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
-        } else {
-            ld_sector(v, static_cast<const uint32_t *>(row) + c);
+    if (!there) return;
+    if constexpr (W == 4) {
+        const uint4 u = *static_cast<const uint4 *>(at);
+        v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
+    } else {
+        ld_sector(v, at);
+    }
+}
+template <int W>
+__device__ __forceinline__ void mx_load_raw(MxRaw<W> &r, const void *at, int n, const void *end)
+{
+    constexpr int kPieces = W == 4 ? 2 : 3, kSize = W == 4 ? 2 : 4;
+    const uintptr_t first = reinterpret_cast<uintptr_t>(at), stop = first + (uintptr_t)(n * kSize), last = reinterpret_cast<uintptr_t>(end);
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+        const uintptr_t a = (first & ~(uintptr_t)15) + 16 * j;
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (n > 0 && a < stop) {
+            if (a + 16 <= last) u = *reinterpret_cast<const uint4 *>(a);
+            else {
+                // the matrix ends inside the piece
+                uint32_t t[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (a + 4 * i + 4 <= last) t[i] = *reinterpret_cast<const uint32_t *>(a + 4 * i);
+                    else if (kSize == 2 && a + 4 * i + 2 <= last) t[i] = *reinterpret_cast<const uint16_t *>(a + 4 * i);
+                }
+                u = make_uint4(t[0], t[1], t[2], t[3]);
+            }
         }
-        return;
+        r.w[4 * j] = u.x; r.w[4 * j + 1] = u.y; r.w[4 * j + 2] = u.z; r.w[4 * j + 3] = u.w;
+    }
+}
+template <int W>
+__device__ __forceinline__ void mx_align(uint32_t (&v)[W], const MxRaw<W> &r, const void *at, int n)
+{
+    constexpr int kN = W == 4 ? 8 : 12;
+    const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(at) & 15u;
+    uint32_t w[kN];
+#pragma unroll
+    for (int i = 0; i < kN; ++i) w[i] = r.w[i];
+    if (off & 8u) {
+#pragma unroll
+        for (int i = 0; i + 2 < kN; ++i) w[i] = w[i + 2];
+    }
+    if (off & 4u) {
+#pragma unroll
+        for (int i = 0; i + 1 < kN; ++i) w[i] = w[i + 1];
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (c + i < cols) {
-            if constexpr (kHalf) v[i / 2] |= (uint32_t)static_cast<const uint16_t *>(row)[c + i] << (16 * (i & 1));
-            else v[i] = static_cast<const uint32_t *>(row)[c + i];
+    for (int i = 0; i < W; ++i) {
+        if constexpr (W == 4) {
+            v[i] = __funnelshift_r(w[i], w[i + 1], 8 * (off & 3u));
+            if (2 * i + 1 >= n) v[i] = 2 * i < n ? v[i] & 0xFFFFu : 0u;
+        } else {
+            v[i] = i < n ? w[i] : 0u;
         }
+    }
 }
 
 // largest magnitude of the eight, the upper half of its bits (infinities and NaN come out above every number)
