@@ -250,23 +250,39 @@ __device__ __forceinline__ void mx_epilogue_slabs(const MxTiles &p, int unit, in
 // ---- epilogue from registers: a lane writes one output of 64 rows of a block -----------------------------------------------------
 // 32 rows of one output: bias + residuals, then sums + those, ReLU, one rounding.  `at`: element of the first row; `n`: rows there are
 // (none where the output lies past the end).  The pointer walks from row to row: 32 addresses at once would not fit beside the sums.
+// The loads of 32 whole rows have no conditions between them and are converted behind the last one (with a condition and a conversion at
+// each 200704x64 -> 250 with residual took 87 us, 68 so, with a 16-bit input 143 and 82).
 template <bool kBf16>
 __device__ __forceinline__ void mx_load_residuals(float (&add)[32], float b, const void *res, int64_t at, int64_t O, int n)
 {
     using T = typename std::conditional<kBf16, uint16_t, float>::type;
     const T *q = static_cast<const T *>(res) + at;
+    T raw[32];
+    if (n >= 32) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        add[i] = 0.f;
-        if (i < n) {
-            if constexpr (kBf16) add[i] = __uint_as_float((uint32_t)__ldg(q) << 16);
-            else add[i] = __ldg(q);
+        for (int i = 0; i < 32; ++i) {
+            raw[i] = __ldg(q);
+            q += O;
+            asm volatile("" : "+l"(q));
         }
-        q += O;
-        asm volatile("" : "+l"(q));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            raw[i] = 0;
+            if (i < n) raw[i] = __ldg(q);
+            q += O;
+            asm volatile("" : "+l"(q));
+        }
     }
 #pragma unroll
-    for (int i = 0; i < 32; ++i) add[i] += b;
+    for (int i = 0; i < 32; ++i) {
+        if constexpr (kBf16) {
+            asm volatile("" : "+h"(raw[i]));
+            add[i] = b + __uint_as_float((uint32_t)raw[i] << 16);
+        } else {
+            add[i] = b + raw[i];
+        }
+    }
 }
 template <bool kBf16>
 __device__ __forceinline__ void mx_store_rows(const uint32_t (&v)[32], const float (&add)[32], void *y, int64_t at, int64_t O, int n, int relu)

@@ -272,7 +272,8 @@ def test_refusals():
 
 @pytest.mark.parametrize("kind,path,variant", [("blob", 4, 128), ("blob", 4, 256), ("blob", 5, 0), ("16", 4, 128), ("16", 4, 256)])
 @pytest.mark.parametrize("M,I,O,res", [(1939, 585, 3768, False), (2500, 2112, 128, True), (4867, 640, 560, True), (1300, 2304, 3128, True), (9000, 64, 328, False),
-                                       (20000, 40, 72, True)])
+                                       (20000, 40, 72, True), (1939, 96, 333, True), (3000, 640, 131, False), (30000, 64, 257, True), (700, 64, 1, True),
+                                       (9000, 40, 7, False), (2500, 2304, 1130, True)])
 def test_outputs_that_end_inside_a_tile_many_times(M, I, O, res, kind, path, variant):
     """Tiles with one half of 64 outputs between tiles with two, blocks of rows that end inside a tile: the order of the slabs shifts
     between the warps that fill them.  Every run has to give the same bits."""
