@@ -338,7 +338,8 @@ npas_status npas_subsample2d(int32_t N, int32_t H, int32_t W, int32_t C, int32_t
  * npas_linear_mx: GEMM with 4-bit weights (w_blob: O rows, I columns), fused epilogue as in npas_linear_bb
  *   Y[m,o] = act(bias[o] + sum_i X[m,i] W[o,i] (+ residual[m,o])), sums in fp32, one rounding to y_dtype; any M, I, O
  *   (O rows of Y and the residual are contiguous).  An infinity or a NaN in a row of X (or a NaN block of W) makes
- *   what it is multiplied into NaN or infinite; other rows (columns) are untouched; ReLU turns a NaN sum into zero.  y may not alias x or the residual.
+ *   what it is multiplied into NaN or infinite; other rows (columns) are untouched; ReLU turns a NaN sum into zero.
+ *   y may not overlap x, w or the residual.
  *   ws_dev: npas_linear_mx_workspace bytes, the first NPAS_WORKSPACE_BYTES zeroed once by the caller before first use (the
  *   status words); its contents need not survive between calls, and calls that may overlap on the GPU (on two streams, in two
  *   graphs) need one each.

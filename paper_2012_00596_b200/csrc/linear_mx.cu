@@ -32,15 +32,15 @@ npas_mx_linear_desc behind_quantize(npas_mx_linear_desc d)
 // Kernel (1: CUDA cores, 3: few rows, 4: persistent tiles, 5: the same on CTA pairs, 6: a 16-bit input of up to 16 rows; 0: none) and variant.
 struct Choice { int kernel, variant; };
 
-// The automatic choice: the kernel, tile or split that a model puts lowest.  Fitted by least squares to 25 000 random layers per kind of input
+// The automatic choice: the kernel, tile or split that a model puts lowest.  Fitted by least squares to 4600 random layers per kind of input
 // (M 17 to 60000, I and O 16 to 8192, a third with residuals, half of odd widths), each timed on every kernel that takes it: standard
-// error 8 to 16 %, the kernel it picks takes 1.4 % (4-bit) and 2 % (16-bit) more than the best one on average.  Microseconds of a launch,
+// error 8 to 15 %, the kernel it picks takes 1.1 % (4-bit) and 1.5 % (16-bit) more than the best one on average, a fifth more in one layer of 100.  Microseconds of a launch,
 // and per round of tiles of a stage of 256 columns (of a step of 64 with a 16-bit input; where the weights stay), of the epilogue, of
 // residuals in slabs, of bf16 outputs that do not leave by TMA, of those with residuals, of fp32 residuals.
 struct Cost { double launch, k, k_stay, round, res, direct, direct_res, f32_res; };
 constexpr Cost kCosts[2][3] = {
-    {{3.66, 0.463, 0.467, 0.72, 0.35, 0.02, 1.30, 0.34}, {2.73, 0.555, 0.738, 2.12, 0.58, 0.05, 1.35, 0.22}, {2.13, 0.359, 0.359, 3.19, 0.64, 0.22, 2.08, 0.47}},
-    {{3.68, 0.268, 0.156, 1.32, 0.33, 0.32, 1.67, 0.43}, {2.84, 0.322, 0.353, 2.73, 0.70, 0.56, 2.18, 0.23}, {}}};
+    {{3.67, 0.405, 0.350, 0.80, 0.36, 0.06, 0.67, 0.35}, {2.87, 0.497, 0.654, 2.06, 0.61, 0.09, 0.90, 0.24}, {2.34, 0.346, 0.346, 3.18, 0.66, 0.24, 1.09, 0.39}},
+    {{3.88, 0.241, 0.160, 1.38, 0.28, 0.35, 0.88, 0.52}, {1.47, 0.356, 0.343, 4.45, 0.92, 0.00, 1.15, 0.00}, {}}};
 
 Choice choose(const npas_mx_linear_desc &d)
 {
@@ -67,15 +67,16 @@ Choice choose(const npas_mx_linear_desc &d)
         for (int ks = 1; ks <= 8; ks *= 2) {
             // (a split is one wave; clusters do not straddle groups of SMs, so larger ones fill less of the chip: 34 of four took two waves)
             if (ks > 1 && (ks > stages || tiles * ks > (ks == 8 ? sms / 2 : ks == 4 ? sms - sms / 9 : sms))) break;
-            const double us = (ks == 1 ? 2.8 : mx ? 2.9 : 3.4) + (double)div(tiles * ks, sms) * ((mx ? 0.306 : 1.04) * (double)div(stages, ks) +
-                                                                (ks == 1 ? 0.019 : 0.039) * rows + (d.has_residual ? (ks == 1 ? 0.031 : 0.004) * rows : 0.));
+            const double per_row = ks == 1 ? (mx ? 0.019 : 0.016) + (d.has_residual ? mx ? 0.032 : 0.019 : 0.)
+                                           : (mx ? 0.042 : 0.033) + (d.has_residual ? mx ? 0.004 : 0.002 : 0.);
+            const double us = (ks == 1 ? mx ? 2.98 : 2.75 : mx ? 2.96 : 3.60) + (double)div(tiles * ks, sms) * ((mx ? 0.304 : 0.88) * (double)div(stages, ks) + per_row * rows);
             consider(3, ks, us);
         }
         if (quantizes_itself(d)) return best;
     }
     // persistent tiles of 128 or 256 rows, and of 256 on CTA pairs
     const bool f32 = d.y_dtype == NPAS_F32, direct = !f32 && d.O % 8 != 0;
-    for (int i = 0; i < (mx && d.I >= 1024 && d.O > 128 ? 3 : 2); ++i) {
+    for (int i = 0; i < (mx && d.O > 128 ? 3 : 2); ++i) {
         const Cost &c = kCosts[mx ? 0 : 1][i];
         const bool pair = i == 2;
         const long long across = div(d.O, pair ? 256 : 128), tiles = div(d.M, i == 0 ? 128 : 256) * across, units = pair ? sms / 2 : sms;

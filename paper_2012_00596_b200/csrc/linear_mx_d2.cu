@@ -1,4 +1,4 @@
-// GEMM of 4-bit inputs with 4-bit weights on CTA pairs (tcgen05 cta_group::2): 256 outputs x N input rows (128 or 256) per MMA.
+// GEMM of 4-bit inputs with 4-bit weights on CTA pairs (tcgen05 cta_group::2): 256 outputs x 256 input rows per MMA.
 //
 // The kernel of linear_mx_ps.cu for inputs that are blobs, with every MMA shared by the two CTAs of a cluster: each CTA has the weights
 // of its own 128 outputs and one half of the input's rows.  A stage of 256 columns is 32 KB per SM instead of 48 with 256 rows: by
@@ -6,7 +6,7 @@
 // the registers of four warps per CTA, a lane quarter each, in groups of five stages: tcgen05.cp on a pair takes 130 cycles for 512
 // bytes and holds up the MMAs behind it (8192^3 261 us with six a stage, 177 with none), and a hand-over between the CTAs per stage
 // takes longer than the stage (620).  Copies of both CTAs complete on the leader's barriers, the leader's warp 1 issues the
-// MMAs and the copies of scales for both and frees stages and hands over accumulators with multicast commits; both CTAs' epilogues
+// MMAs for both and frees stages and hands over accumulators with multicast commits; both CTAs' epilogues
 // (mx_epi.cuh) read their own 128 lanes; the peer's hand the accumulator back through one arrival with release semantics at cluster
 // scope by its warp 1, as in linear_d2.cu.  Every wait is bounded; a role that gives up raises the abort flag of both CTAs.
 #include "mx_epi.cuh"

@@ -3,7 +3,7 @@
 // Y[m,o] = act(bias[o] + sum_i X[m,i] W[o,i] + residual[m,o]).  With so few rows nothing is read twice, so the weights go from memory
 // to registers, are widened there and multiplied by warp-wide MMAs (m16n8k16, fp32 sums): no stage, barrier or tensor-memory hand-over between
 // the load and the product (linear_mx_sw.cu, whose tensor-core MMAs take the weights from tensor memory, is held up by those: 1x8192 -> 8192
-// 20.7 us, FIXME here).  The order of the columns in an MMA is free as long as both operands agree: a thread takes a whole block of 32
+// 20.7 us, 12.7 here).  The order of the columns in an MMA is free as long as both operands agree: a thread takes a whole block of 32
 // columns of a row (16 bytes) and one scale, and of X the same 32 columns (64 bytes) of one row, each exactly as it lies in memory.
 // A block of threads has 32 outputs (8a + g, + 32, + 64, + 96 of a tile of scales, whose 16 bytes hold those four rows), a warp every
 // sixteenth tile of 128 columns of them; the warps' sums meet in shared memory and are added in order.  2.1 instructions a weight,

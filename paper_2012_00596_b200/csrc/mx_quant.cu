@@ -110,15 +110,15 @@ __global__ void __launch_bounds__(kThreads) quantize_mx_kernel(int rows, int col
 template <typename T>
 __device__ __forceinline__ void store8(T *row, int c, const float (&v)[8])
 {
-        if constexpr (sizeof(T) == 2) {
-            *reinterpret_cast<uint4 *>(row + c) = make_uint4(tc::cvt_bf16x2(v[0], v[1]), tc::cvt_bf16x2(v[2], v[3]), tc::cvt_bf16x2(v[4], v[5]),
-                                                             tc::cvt_bf16x2(v[6], v[7]));
-        } else {
-            uint32_t o[8];
+    if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<uint4 *>(row + c) = make_uint4(tc::cvt_bf16x2(v[0], v[1]), tc::cvt_bf16x2(v[2], v[3]), tc::cvt_bf16x2(v[4], v[5]),
+                                                         tc::cvt_bf16x2(v[6], v[7]));
+    } else {
+        uint32_t o[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(v[i]);
-            tc::st_sector(row + c, o);
-        }
+        for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(v[i]);
+        tc::st_sector(row + c, o);
+    }
 }
 
 // (element times 2^126, then times the scale: both exact; every value is a bf16 number too, subnormals included)
