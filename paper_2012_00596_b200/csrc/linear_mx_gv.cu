@@ -3,11 +3,13 @@
 // Y[m,o] = act(bias[o] + sum_i X[m,i] W[o,i] + residual[m,o]).  With so few rows nothing is read twice, so the weights go from memory
 // to registers, are widened there and multiplied by warp-wide MMAs (m16n8k16, fp32 sums): no stage, barrier or tensor-memory hand-over between
 // the load and the product (linear_mx_sw.cu, whose tensor-core MMAs take the weights from tensor memory, is held up by those: 1x8192 -> 8192
-// 20.7 us, 12.7 here).  The order of the columns in an MMA is free as long as both operands agree: a thread takes a whole block of 32
+// 20.7 us, 12.1 here).  The order of the columns in an MMA is free as long as both operands agree: a thread takes a whole block of 32
 // columns of a row (16 bytes) and one scale, and of X the same 32 columns (64 bytes) of one row, each exactly as it lies in memory.
 // A block of threads has 32 outputs (8a + g, + 32, + 64, + 96 of a tile of scales, whose 16 bytes hold those four rows), a warp every
-// sixteenth tile of 128 columns of them; the warps' sums meet in shared memory and are added in order.  2.1 instructions a weight,
-// at the issue rate 60 weights a cycle and SM, HBM delivers 46.
+// sixteenth tile of 128 columns of them; the warps' sums meet in shared memory and are added in order.  Bound by the SMs' logic pipe (nine of
+// the 17 instructions that widen eight weights, half of them a cycle; 66 % busy where two blocks share an SM) and the two microseconds that a
+// launch, its first loads and its last sums take.  Copies into a ring in shared memory, three shares ahead, cost more instructions than the
+// wait that they save (1x8192 -> 8192 17.2 us).
 #include "mx_tc.cuh"
 
 namespace npas {
@@ -45,32 +47,45 @@ linear_mx_gv_kernel(int M, int I, int O, int relu, int y_bf16, int nKT, uint32_t
     pdl_wait();
     x = behind_wait(x); w = behind_wait(w); bias = behind_wait(bias); res = behind_wait(res);
     float c[2][NT][4] = {};
-    const int row0 = ot * kMxTileRows + a8 + g;
-    const uint8_t *e0 = w + off_values + (uint64_t)row0 * pitch + q * (kMxBlock / 2);
-    const uint4 *s0 = reinterpret_cast<const uint4 *>(w + off_scales + (uint64_t)ot * nKT * kMxScaleTile) + a8 + g;
-    const uint16_t *x0 = x + (int64_t)g * x_pitch + q * kMxBlock;
-    auto load = [&](Share &v, int kt) {
-        const int left = I - (kt * kMxTileCols + q * kMxBlock);            // columns there are from this thread's first one on
-        v.codes = __ldg(s0 + (int64_t)kt * (kMxScaleTile / 16));
+    // Rows past the end are the last one again: what they give is not stored.  Offsets from the tile's first byte, and from X, fit in 32 bits.
+    const uint8_t *wt = w + off_values + (uint64_t)ot * kMxTileRows * pitch;
+    const uint8_t *st = w + off_scales + (uint64_t)ot * nKT * kMxScaleTile;
+    const uint8_t *xb = reinterpret_cast<const uint8_t *>(x);
+    uint32_t row[4], x_row[NT];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            v.e[j] = row0 + 32 * j < O && left > 0 ? __ldg(reinterpret_cast<const uint4 *>(e0 + (uint64_t)(32 * j) * pitch + (uint32_t)kt * (kMxTileCols / 2)))
-                                                   : make_uint4(0, 0, 0, 0);
+    for (int j = 0; j < 4; ++j) row[j] = (uint32_t)min(32 * j + a8 + g, O - 1 - ot * kMxTileRows) * pitch + q * (kMxBlock / 2);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) x_row[t] = (uint32_t)min(t * 8 + g, M - 1) * (uint32_t)x_pitch * 2u + q * (kMxBlock * 2);
+    const uint32_t code_row = (uint32_t)(a8 + g) * 16u, pick = 0x4440u | (uint32_t)q;
+    const int nW = I / kMxTileCols;                            // tiles without an end inside
+    auto load = [&](Share &v, int kt) {
+        v.codes = __ldg(reinterpret_cast<const uint4 *>(st + (uint32_t)kt * kMxScaleTile + code_row));
+        const bool in = kt < nW || I - (kt * kMxTileCols + q * kMxBlock) > 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v.e[j] = make_uint4(0, 0, 0, 0);
+            if (in) v.e[j] = __ldg(reinterpret_cast<const uint4 *>(wt + (row[j] + (uint32_t)kt * (kMxTileCols / 2))));
+        }
     };
     auto load_x = [&](ShareX<NT> &v, int kt) {
-        const int left = I - (kt * kMxTileCols + q * kMxBlock);
+        const int left = I - (kt * kMxTileCols + q * kMxBlock);            // columns there are from this thread's first one on
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t) {
+            const uint4 *from = reinterpret_cast<const uint4 *>(xb + (x_row[t] + (uint32_t)kt * (kMxTileCols * 2)));
+            if (kt < nW) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                v.x[t][i] = t * 8 + g < M && 8 * i < left ? __ldg(reinterpret_cast<const uint4 *>(x0 + (int64_t)t * 8 * x_pitch + kt * kMxTileCols) + i)
-                                                          : make_uint4(0, 0, 0, 0);
+                for (int i = 0; i < 4; ++i) v.x[t][i] = __ldg(from + i);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v.x[t][i] = 8 * i < left ? __ldg(from + i) : make_uint4(0, 0, 0, 0);
+            }
+        }
     };
     auto multiply = [&](const Share &v, const ShareX<NT> &vx) {
         uint32_t code[4], f[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            code[j] = (j == 0 ? v.codes.x : j == 1 ? v.codes.y : j == 2 ? v.codes.z : v.codes.w) >> (8 * q) & 255u;
+            code[j] = __byte_perm(j == 0 ? v.codes.x : j == 1 ? v.codes.y : j == 2 ? v.codes.z : v.codes.w, 0, pick);
             f[j] = mx_factor(code[j]).first;
         }
         const bool large = __any_sync(0xFFFFFFFFu, max(max(code[0], code[1]), max(code[2], code[3])) > 128u);
