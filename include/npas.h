@@ -191,7 +191,7 @@ typedef struct {
  * variant of that kernel that runs on CTA pairs (cta_group::2; 4-bit inputs), 6 = force the kernel
  * for up to 16 rows of a 16-bit input (NPAS_ERR_UNSUPPORTED when the geometry is outside the requested kernel's envelope). */
 typedef struct {
-    int32_t M, I, O;
+    int32_t M, I, O; /* M and O up to 2^31 - 256, I up to 2^20 */
     int32_t x_dtype, quantize_x, y_dtype;
     int32_t relu, has_bias, has_residual;
     int32_t path;

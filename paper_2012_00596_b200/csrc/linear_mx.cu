@@ -13,6 +13,7 @@ npas_status check_args(const npas_mx_linear_desc *d)
     npas_status s = check_mx_desc(&w);
     if (s == NPAS_OK) s = check_mx_desc(&x);
     if (s != NPAS_OK) return s;
+    if (d->M > 0x7FFFFF00 || d->O > 0x7FFFFF00) return NPAS_ERR_SHAPE;         // (rounded up to a tile of 256 they are ints)
     if (d->x_dtype != NPAS_BF16 && d->x_dtype != NPAS_MX4) return NPAS_ERR_DTYPE;
     if (d->quantize_x && d->x_dtype != NPAS_BF16) return NPAS_ERR_DTYPE;
     if (d->y_dtype != NPAS_F32 && d->y_dtype != NPAS_BF16) return NPAS_ERR_DTYPE;

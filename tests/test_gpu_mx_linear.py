@@ -161,6 +161,22 @@ def test_single_row_equals_the_row_of_a_batch_in_exact_arithmetic():
             assert torch.equal(npas.linear_mx(x[:n].contiguous(), w, quantize_x=q, out_dtype=torch.float32), full[:n])
 
 
+@pytest.mark.parametrize("kind,M,I,O,out_dtype,res", [("blob", 264000, 32, 8200, torch.bfloat16, True), ("16", 264000, 32, 8200, torch.bfloat16, False),
+                                                     ("44", 264000, 32, 8195, torch.bfloat16, True), ("16", 264000, 32, 8195, torch.float32, False),
+                                                     ("16", 264000, 8195, 40, torch.bfloat16, False), ("44", 264000, 8200, 40, torch.bfloat16, False)])
+def test_offsets_past_32_bits(kind, M, I, O, out_dtype, res):
+    """Whole numbers: the last rows of inputs and outputs of more than 2^31 elements are those of a call of them alone."""
+    g = torch.Generator(device="cuda").manual_seed(4)
+    few = lambda lo, hi, *size: torch.randint(lo, hi, size, generator=g, device="cuda", dtype=torch.int8)
+    x, w = few(-2, 3, M, I).to(torch.bfloat16), npas.quantize_mx(few(-2, 3, O, I).to(torch.bfloat16))
+    r = few(-2, 3, M, O).to(out_dtype) if res else None
+    f = lambda x, r: npas.linear_mx(npas.quantize_mx(x) if kind == "blob" else x, w, None, r, out_dtype=out_dtype, quantize_x=kind == "44")
+    y = f(x, r)
+    assert y.numel() > 2 ** 31 or x.numel() > 2 ** 31
+    for lo, n in ((M - 300, 300), (M - 1, 1), (2 ** 31 // max(I, O), 200), (0, 100)):
+        assert torch.equal(y[lo:lo + n], f(x[lo:lo + n].clone(), None if r is None else r[lo:lo + n].clone())), lo
+
+
 def test_rows_behind_the_last_are_left_alone():
     for M, O in ((1, 40), (33, 129), (200, 264), (5, 1001)):
         c = _case(M, 96, O, res=False)

@@ -150,3 +150,14 @@ def test_refusals():
     with pytest.raises(npas.NpasError) as e:
         npas.blob_check(spoilt)
     assert e.value.code == 6
+
+
+@pytest.mark.parametrize("rows,cols,dtype", [(262400, 16400, torch.bfloat16), (262400, 16397, torch.bfloat16), (140000, 16397, torch.float32)])
+def test_offsets_past_32_bits(rows, cols, dtype):
+    """More than 2^31 elements (of bf16 2^32): the last rows, and those around 2^31 and 2^32 elements, come back as they do alone."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x = torch.randint(-100, 101, (rows, cols), generator=g, device="cuda", dtype=torch.int8).to(dtype)
+    y = npas.dequantize_mx(npas.quantize_mx(x), dtype)
+    for lo in (0, 2 ** 31 // cols - 50, min(2 ** 32 // cols - 50, rows - 300), rows - 100):
+        part = x[lo:lo + 100].clone()
+        assert torch.equal(y[lo:lo + 100], npas.dequantize_mx(npas.quantize_mx(part), dtype)), lo

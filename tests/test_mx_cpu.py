@@ -69,7 +69,7 @@ def _linear(lib, ws=256, x=4096, w=8192, bias=0, res=0, y=16384, wsp=32768, **kw
 
 @pytest.mark.parametrize("kw,code", [
     (dict(x=0), 1), (dict(w=0), 1), (dict(y=0), 1), (dict(wsp=0), 1), (dict(has_bias=1), 1), (dict(has_residual=1), 1),
-    (dict(M=0), 2), (dict(I=0), 2), (dict(O=-4), 2), (dict(I=2 ** 20 + 1), 2),
+    (dict(M=0), 2), (dict(M=2 ** 31 - 255), 2), (dict(O=2 ** 31 - 1), 2), (dict(I=0), 2), (dict(O=-4), 2), (dict(I=2 ** 20 + 1), 2),
     (dict(x_dtype=0), 3), (dict(x_dtype=2, quantize_x=1), 3), (dict(y_dtype=2), 3),
     (dict(x=4104), 4), (dict(w=8200), 4), (dict(y=16392), 4), (dict(has_bias=1, bias=20), 4), (dict(has_residual=1, res=24), 4),
     (dict(ws=255), 7), (dict(quantize_x=1, M=400), 7), (dict(y=4096), 8), (dict(y=8192), 8), (dict(has_residual=1, res=16384), 8), (dict(path=99), 8)])
