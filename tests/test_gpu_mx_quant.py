@@ -153,7 +153,7 @@ def test_refusals():
 
 
 @pytest.mark.parametrize("rows,cols,dtype", [(262400, 16400, torch.bfloat16), (262400, 16397, torch.bfloat16), (140000, 16397, torch.float32)])
-def test_offsets_past_32_bits(rows, cols, dtype):
+def test_many_elements_both_ways(rows, cols, dtype):
     """More than 2^31 elements (of bf16 2^32): the last rows, and those around 2^31 and 2^32 elements, come back as they do alone."""
     g = torch.Generator(device="cuda").manual_seed(6)
     x = torch.randint(-100, 101, (rows, cols), generator=g, device="cuda", dtype=torch.int8).to(dtype)
