@@ -102,6 +102,12 @@ def test_larger_sizes(M, I, O, kind):
     _run(M, I, O, kind, relu=True, seed=3)
 
 
+@pytest.mark.parametrize("M,I,O", [(1, 8192, 1024), (9, 8000, 300), (3, 16384, 130), (16, 4999, 500), (8, 4096, 1), (2, 8200, 2048)])
+def test_few_rows_of_few_outputs_and_many_columns(M, I, O):
+    """A cluster splits the columns; the last part may be shorter, or have no tile for some warps."""
+    _run(M, I, O, "16", relu=True, seed=8, spread=1)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("M", list(range(1, 18)) + [24, 31, 32, 40, 63, 65, 96, 120, 136, 192, 255, 257])
 def test_every_count_of_rows(M, kind):
