@@ -8,6 +8,8 @@
 // Where the tiles of a CTA all have the same outputs (the grid is a multiple of the tiles across) and their weights fit, the weights stay: a
 // 4-bit input's in shared memory (their copies were half of a small tile's), a 16-bit input's widened in tensor memory.
 // Outputs leave by mx_epi.cuh.  Every wait is bounded.
+#include <type_traits>
+
 #include "mx_epi.cuh"
 
 namespace npas {
@@ -18,7 +20,7 @@ namespace {
 
 constexpr int kRows = 128;
 constexpr int kStepCols = 256;                             // columns of a weight stage
-constexpr int kMaxStages = 6, kMaxXStages = 4, kSlots = 4;
+constexpr int kMaxStages = 6, kMaxXStages = 8, kSlots = 4;
 constexpr uint32_t kSlotCols = 64;                         // tensor memory of a slot: 128 widened columns of the weights
 constexpr uint32_t kSmemLimit = 232448;
 constexpr uint32_t kWBytes = kRows * 128;
@@ -29,7 +31,7 @@ constexpr uint32_t kWStage = kWBytes + kScaleBytes;
 template <bool kMx> struct Roles {
     static constexpr int kXWarp = 2, kWideWarps = kMx ? 0 : 8, kFirstWide = 3;
     static constexpr int kFirstEpi = kMx ? 2 : kFirstWide + kWideWarps + 1;
-    static constexpr int kEpiWarps = kMx ? 16 : 8, kGroups = kEpiWarps / 8;
+    static constexpr int kEpiWarps = kMx ? 16 : 8;
     static constexpr int kStoreWarp = kMx ? kFirstEpi + kEpiWarps : kFirstWide + kWideWarps;
     static constexpr int kThreads = (kFirstEpi + kEpiWarps + (kMx ? 1 : 0)) * 32;
 };
@@ -65,13 +67,16 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
     volatile uint32_t *abort_flag = &bars->abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int nK = (p.I + 63) / 64;                        // K steps of 64 columns
+    // Outputs leave from registers and the widening is over after the first tile: its warps are the epilogue's second group (50000x64 -> 333 18.8 ->
+    // 16.4 us, 200704x256 -> 250 with residual 87 -> 78; outputs that leave by TMA gain nothing by it, 200704x64 -> 256 33.1 -> 35.0)
+    const bool helped = !kMx && p.resident && !p.t.NS;
 
     if (tid == 0) {
         for (int s = 0; s < p.S; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], kMx ? 1 : R::kWideWarps); }
         for (int s = 0; s < p.SX; ++s) { mbar_init(&bars->x_full[s], 1); mbar_init(&bars->x_empty[s], 1); }
         for (int s = 0; s < p.slots; ++s) { mbar_init(&bars->slot_full[s], 4); mbar_init(&bars->slot_empty[s], 1); }
         mbar_init(&bars->w_full, 1);
-        mx_epi_init(&bars->epi, p.t, p.t.acc == 2 ? 8 : R::kEpiWarps);
+        mx_epi_init(&bars->epi, p.t, p.t.acc == 2 || !(kMx || helped) ? 8 : 16);
         bars->abort_flag = 0;
         fence_barrier_init();
         prefetch_tensormap(&tmap_x);
@@ -86,6 +91,17 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
     const uint32_t tmem_base = bars->tmem_base;
     pdl_wait();
     bias = behind_wait(bias); res = behind_wait(res);
+
+    auto release = [&](uint32_t acc) {
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->epi.acc_empty[acc]);
+    };
+    // warp e of the epilogue's, where outputs leave from registers
+    auto rows = [&](auto groups, int e) {
+        mx_epilogue_rows<decltype(groups)::value, kBf16>(p.t, blockIdx.x, 0, e, lane, warp & 3, tmem_base, &bars->epi, bias, res, y, abort_flag, ws, release);
+    };
+    const std::integral_constant<int, 2> two;
 
     if (warp == 0) {
         if (lane == 0) {
@@ -285,19 +301,17 @@ linear_mx_ps_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
                 if (++s == (uint32_t)p.S) { s = 0; ph ^= 1u; }
             }
         }
+        if (helped) rows(two, 8 + warp - R::kFirstWide);
     } else if (warp == R::kStoreWarp) {
         if (lane == 0 && p.t.NS) mx_slab_copies(p.t, blockIdx.x, 0, smem, &bars->epi, &tmap_y, &tmap_r, res != nullptr, abort_flag, ws);
     } else if (warp >= R::kFirstEpi) {
-        auto release = [&](uint32_t acc) {
-            tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bars->epi.acc_empty[acc]);
-        };
+        const std::integral_constant<int, R::kEpiWarps / 8> groups;
+        const int e = warp - R::kFirstEpi;
         if (kBf16 && p.t.NS)
-            mx_epilogue_slabs<R::kGroups, false>(p.t, blockIdx.x, 0, warp - R::kFirstEpi, lane, warp & 3, smem_u32(smem), tmem_base, &bars->epi, bias, res != nullptr, abort_flag,
-                                          ws, release);
-        else
-            mx_epilogue_rows<R::kGroups, kBf16>(p.t, blockIdx.x, 0, warp - R::kFirstEpi, lane, warp & 3, tmem_base, &bars->epi, bias, res, y, abort_flag, ws, release);
+            mx_epilogue_slabs<decltype(groups)::value, false>(p.t, blockIdx.x, 0, e, lane, warp & 3, smem_u32(smem), tmem_base, &bars->epi, bias, res != nullptr, abort_flag, ws,
+                                                              release);
+        else if (helped) rows(two, e);
+        else rows(groups, e);
     }
     tc_fence_before_sync();
     __syncthreads();
@@ -338,17 +352,22 @@ bool plan(const npas_mx_linear_desc &d, MxPsParams &p, int sms)
     p.stage_bytes = p.x_in_stage + (mx ? p.xs_bytes + p.x_bytes : 0u);
     const uint32_t budget = kSmemLimit - (uint32_t)sizeof(MxPsBars) - 128u - 1024u;
     // Slabs for bf16 outputs with rows on 16-byte boundaries: two where the loads need the room (256 rows of X in 16 bits, or without residuals), else four, eight where
-    // residuals are ahead of little else; and the input's ring
-    p.t.NS = !p.y_bf16 || d.O % 8 ? 0 : N == 256 && (!mx || (p.nS > 2 && !d.has_residual)) ? 2 : mx && d.has_residual && p.nS <= 2 && N == 128 ? 8 : 4;
+    // residuals are ahead of little else (200704x64 -> 256 with residual, 16-bit input 43.0 us with four, 39.9); and the input's ring
+    p.t.NS = !p.y_bf16 || d.O % 8 ? 0 : N == 256 && (!mx || (p.nS > 2 && !d.has_residual)) ? 2 : (mx ? d.has_residual && p.nS <= 2 : p.resident && nK <= 2) && N == 128 ? 8 : 4;
     while ((1 << p.t.ns_log) < p.t.NS) ++p.t.ns_log;
     p.slots = mx ? 0 : p.resident ? (nK + 1) / 2 : kSlots;
-    p.x_steps = N == 256 ? 1 : 2;
-    if (!mx) p.SX = N == 256 ? 4 : 3;
-    const uint32_t fixed = p.off_stages + (uint32_t)(p.SX * p.x_steps) * p.x_bytes + (uint32_t)p.t.NS * kMxSlabBytes;
+    p.x_steps = N == 256 || (p.resident && nK == 1) ? 1 : 2;
+    const uint32_t slabs = (uint32_t)p.t.NS * kMxSlabBytes;
+    if (!mx) {
+        // (weights that stay need their stages once: the room is the input's)
+        p.SX = N == 256 ? 4 : 3;
+        if (p.resident) p.SX = min(kMaxXStages, (int)((budget - slabs - (uint32_t)p.nS * p.stage_bytes) / ((uint32_t)p.x_steps * p.x_bytes)));
+    }
+    const uint32_t fixed = p.off_stages + (uint32_t)(p.SX * p.x_steps) * p.x_bytes + slabs;
     if (fixed >= budget) return false;
     p.S = (int)((budget - fixed) / p.stage_bytes);
     if (p.S > kMaxStages) p.S = kMaxStages;
-    if (p.S < 2) return false;
+    if (p.S < (p.resident ? 1 : 2)) return false;
     p.off_x = p.off_stages + (uint32_t)p.S * p.stage_bytes;
     p.t.off_slabs = p.off_x + (uint32_t)(p.SX * p.x_steps) * p.x_bytes;
     p.off_bar = round_up(p.t.off_slabs + (uint32_t)p.t.NS * kMxSlabBytes, 128);
