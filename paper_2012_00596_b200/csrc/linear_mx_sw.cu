@@ -13,6 +13,8 @@
 //     MMAs of kind::f16 take their first operand.  Slots of two steps; weights and inputs have rings of their own (256 and 128 columns a
 //     stage).  Widening costs 2.4 instructions a weight, at the issue rate about what HBM delivers.
 // Every wait is bounded.
+#include <type_traits>
+
 #include "mx_tc.cuh"
 #include "tc_pair.cuh"
 
@@ -275,26 +277,38 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
     const int rows = min(p.N, p.M - mt * p.N);                 // rows of X in this tile (with a 4-bit input several tiles are of 128)
     if (p.KS > 1) cluster_wait();      // every CTA of the cluster is running
     if (warp >= 2 && warp < kXWarp && s_n > 0) {
+        constexpr int kStride = 16 * (kEpiWarps / 4);
         const int quarter = warp & 3, part = (warp - 2) >> 2, o = ot * kRows + quarter * 32 + lane;
+        const bool direct = p.KS == 1;
+        // Residuals of 16 rows, asked for before the sums are there and, from the second 16 on, while the ones before are written.  Loads without
+        // conditions (rows past the last are the last one), converted when they are used: else each waits for the one before
+        typename std::conditional<kBf16, uint16_t, float>::type ahead[16];
+        auto load_ahead = [&](int c0) {
+            const int n = o < p.O ? rows - c0 : 0;
+            if (!direct || !res || n <= 0) return;
+            const auto *from = static_cast<const std::remove_reference_t<decltype(ahead[0])> *>(res) + ((int64_t)(mt * p.N + c0) * p.O + o + z);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) ahead[i] = __ldg(from + (int64_t)min(i, n - 1) * p.O);
+        };
+        load_ahead(part * 16);
         if (__all_sync(0xFFFFFFFFu, mbar_wait(&bars->acc_full, 0, abort_flag, ws, 0xA500))) {
             tc_fence_after_sync();
             const uint32_t t_addr = tmem_base + ((uint32_t)(quarter * 32) << 16);
-            const float b = p.KS == 1 && bias && o < p.O ? __ldg(bias + o + z) : 0.f;
-            for (int c0 = part * 16; c0 < rows; c0 += 16 * (kEpiWarps / 4)) {
+            const float b = direct && bias && o < p.O ? __ldg(bias + o + z) : 0.f;
+            for (int c0 = part * 16; c0 < rows; c0 += kStride) {
                 uint32_t v[16];
                 __syncwarp();
                 tmem_ld_x16(t_addr + c0, v);
-                if (p.KS == 1) {
+                if (direct) {
                     const int64_t at = (int64_t)(mt * p.N + c0) * p.O + o + z;
                     const int n = o < p.O ? rows - c0 : 0;
                     float add[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) add[i] = 0.f;
-                    if (res) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (i < n) add[i] = load_res<kBf16>(res, at + (int64_t)i * p.O);
+                    for (int i = 0; i < 16; ++i) {
+                        if constexpr (kBf16) add[i] = res ? bf16_bits_to_f32(ahead[i]) : 0.f;
+                        else add[i] = res ? ahead[i] : 0.f;
                     }
+                    load_ahead(c0 + kStride);
                     tmem_ld_wait();
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
