@@ -33,15 +33,15 @@ npas_mx_linear_desc behind_quantize(npas_mx_linear_desc d)
 // Kernel (1: CUDA cores, 3: few rows, 4: persistent tiles, 5: the same on CTA pairs, 6: a 16-bit input of up to 16 rows; 0: none) and variant.
 struct Choice { int kernel, variant; };
 
-// The automatic choice: the kernel, tile or split that a model puts lowest.  Fitted by least squares to 4600 random layers per kind of input
+// The automatic choice: the kernel, tile or split that a model puts lowest.  Fitted by least squares to 14700 random layers per kind of input
 // (M 17 to 60000, I and O 16 to 8192, a third with residuals, half of odd widths), each timed on every kernel that takes it: standard
-// error 8 to 15 %, the kernel it picks takes 1.1 % (4-bit) and 1.5 % (16-bit) more than the best one on average, a fifth more in one layer of 100.  Microseconds of a launch,
+// error 7 to 15 %, the kernel it picks takes 1.0 % (4-bit) and 1.3 % (16-bit) more than the best one on average, a fifth more in one layer of 100.  Microseconds of a launch,
 // and per round of tiles of a stage of 256 columns (of a step of 64 with a 16-bit input; where the weights stay), of the epilogue, of
 // residuals in slabs, of bf16 outputs that do not leave by TMA, of those with residuals, of fp32 residuals.
 struct Cost { double launch, k, k_stay, round, res, direct, direct_res, f32_res; };
 constexpr Cost kCosts[2][3] = {
-    {{3.67, 0.405, 0.350, 0.80, 0.36, 0.06, 0.67, 0.35}, {2.87, 0.497, 0.654, 2.06, 0.61, 0.09, 0.90, 0.24}, {2.34, 0.346, 0.346, 3.18, 0.66, 0.24, 1.09, 0.39}},
-    {{3.88, 0.241, 0.160, 1.38, 0.28, 0.35, 0.88, 0.52}, {1.47, 0.356, 0.343, 4.45, 0.92, 0.00, 1.15, 0.00}, {}}};
+    {{3.29, 0.405, 0.331, 0.90, 0.36, 0.00, 0.58, 0.04}, {2.25, 0.474, 0.598, 2.36, 0.47, 0.00, 0.65, 0.00}, {1.78, 0.344, 0.344, 3.46, 0.52, 0.00, 0.79, 0.14}},
+    {{3.52, 0.245, 0.164, 1.43, 0.25, 0.11, 0.79, 0.13}, {0.87, 0.351, 0.352, 4.61, 0.62, 0.00, 0.90, 0.00}, {}}};
 
 Choice choose(const npas_mx_linear_desc &d)
 {
@@ -68,9 +68,8 @@ Choice choose(const npas_mx_linear_desc &d)
         for (int ks = 1; ks <= 8; ks *= 2) {
             // (a split is one wave; clusters do not straddle groups of SMs, so larger ones fill less of the chip: 34 of four took two waves)
             if (ks > 1 && (ks > stages || tiles * ks > (ks == 8 ? sms / 2 : ks == 4 ? sms - sms / 9 : sms))) break;
-            const double per_row = ks == 1 ? (mx ? 0.019 : 0.016) + (d.has_residual ? mx ? 0.032 : 0.019 : 0.)
-                                           : (mx ? 0.042 : 0.033) + (d.has_residual ? mx ? 0.004 : 0.002 : 0.);
-            const double us = (ks == 1 ? mx ? 2.98 : 2.75 : mx ? 2.96 : 3.60) + (double)div(tiles * ks, sms) * ((mx ? 0.304 : 0.88) * (double)div(stages, ks) + per_row * rows);
+            const double per_row = ks == 1 ? (mx ? 0.027 : 0.022) + (d.has_residual ? 0.006 : 0.) : (mx ? 0.042 : 0.032) + (d.has_residual ? 0.004 : 0.);
+            const double us = (ks == 1 ? 2.49 : mx ? 2.81 : 3.49) + (double)div(tiles * ks, sms) * ((mx ? 0.308 : 0.88) * (double)div(stages, ks) + per_row * rows);
             consider(3, ks, us);
         }
         if (quantizes_itself(d)) return best;
