@@ -88,6 +88,14 @@ def test_pruned_weights_stay_zero():
     assert (kept == 0).sum() >= 128 * 128 * 3 // 4 and bool((v[kept == 0] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [5, 150, 5000])
+def test_rows_that_start_anywhere(rows, dtype):
+    """Every remainder of the columns: rows begin and end at every place of a 16-byte piece, inside a tile of columns and past one."""
+    for cols in list(range(1, 18)) + [57, 62, 63, 64, 65] + list(range(121, 138)) + [257, 259, 262]:
+        _check(_matrix(rows, cols, dtype, seed=cols), DTYPES[dtype])
+
+
 def test_large_matrix_in_pieces():
     """70 000 rows: row tiles past 2^9, values past 16 MB; every 128-row piece equals the quantised piece."""
     x = torch.randn(70001, 512, device="cuda").to(torch.bfloat16)
