@@ -59,8 +59,9 @@ Choice choose(const npas_mx_linear_desc &d)
         if (kernel == 3 ? !linear_mx_sw_supported(t) : kernel == 4 ? !linear_mx_ps_supported(t) : !linear_mx_d2_supported(t)) return;
         best = {kernel, variant}; least = us;
     };
-    // (a few rows more than eight of few columns are left to the tensor cores: 14x48 -> 1042 4.2 us against 3.7)
-    if (linear_mx_gv_supported(in) && (d.M <= 8 || d.I > 128)) return {6, 0};
+    // (a few rows more than eight of few columns are left to the tensor cores: 14x48 -> 1042 4.2 us against 3.7.  Path 2 asks for
+    // the kernels of tcgen05 MMAs; this one's are warp-wide)
+    if (d.path != 2 && linear_mx_gv_supported(in) && (d.M <= 8 || d.I > 128)) return {6, 0};
     // few rows: a CTA, or a cluster that splits the columns, per 128 outputs and up to 128 rows
     if (d.M <= 1024) {
         const long long tiles = div(d.M, 128) * div(d.O, 128);
