@@ -269,7 +269,8 @@ def mask_bb_from_dense(dense_mask: torch.Tensor, Bo: int, Bi: int):
 def blob_check(blob) -> None:
     lib = load()
     if isinstance(blob, MxBlob):
-        _check(lib.npas_mx_blob_check(ctypes.byref(blob.desc), _p(blob.data), ctypes.c_size_t(blob.data.numel()), _stream()), "npas_mx_blob_check")
+        with torch.cuda.device_of(blob.data):
+            _check(lib.npas_mx_blob_check(ctypes.byref(blob.desc), _p(blob.data), ctypes.c_size_t(blob.data.numel()), _stream()), "npas_mx_blob_check")
         return
     bp = ctypes.byref(blob.desc) if isinstance(blob, BpBlob) else None
     bb = ctypes.byref(blob.desc) if isinstance(blob, BbBlob) else None
@@ -458,7 +459,8 @@ def linear_mx_kernel(M: int, w: MxBlob, *, dtype=torch.bfloat16, out_dtype=torch
     """npas_linear_mx_kernel: id of the kernel the call would run (host only; raises NpasError(8) where the path declines)."""
     d = _mx_linear_desc(M, w, dtype, out_dtype, quantize_x, relu, bias, residual, path, variant)
     kid = ctypes.c_int32(0)
-    _check(load().npas_linear_mx_kernel(ctypes.byref(d), ctypes.byref(kid)), "npas_linear_mx_kernel")
+    with torch.cuda.device_of(w.data):                         # (the choice counts that device's SMs)
+        _check(load().npas_linear_mx_kernel(ctypes.byref(d), ctypes.byref(kid)), "npas_linear_mx_kernel")
     return kid.value
 
 
@@ -467,7 +469,8 @@ def linear_mx_workspace(M: int, w: MxBlob, *, dtype=torch.bfloat16, out_dtype=to
     """npas_linear_mx_workspace: device scratch for calls of up to these sizes (status words zeroed), on w's device."""
     d = _mx_linear_desc(M, w, dtype, out_dtype, quantize_x, relu, bias, residual, path, variant)
     n = ctypes.c_size_t(0)
-    _check(load().npas_linear_mx_workspace(ctypes.byref(d), ctypes.byref(n)), "npas_linear_mx_workspace")
+    with torch.cuda.device_of(w.data):
+        _check(load().npas_linear_mx_workspace(ctypes.byref(d), ctypes.byref(n)), "npas_linear_mx_workspace")
     ws = torch.empty(n.value, dtype=torch.uint8, device=w.data.device)
     ws[:WORKSPACE_BYTES].zero_()
     return ws

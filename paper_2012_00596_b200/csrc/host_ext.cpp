@@ -678,10 +678,10 @@ PyObject *linear_mx(PyObject *, PyObject *const *a, Py_ssize_t n)
             fail_assert("w and ws (uint8) must be contiguous on x's device");
             return nullptr;
         }
+        const c10::cuda::CUDAGuard guard(dev);                 // (before the workspace: its size follows from the kernel chosen for the device)
         size_t need = 0;
         s = npas_linear_mx_workspace(&d, &need);
         if (s != NPAS_OK) return PyLong_FromLong((long)s);
-        const c10::cuda::CUDAGuard guard(dev);
         at::Tensor made, own, scratch;
         void *status = nullptr, *sp = nullptr;
         size_t sb = 0;

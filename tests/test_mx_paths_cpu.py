@@ -26,3 +26,34 @@ def test_path_2_names_tcgen05_kernels_only(M, I, O, dtype, quantize):
     assert kid in TENSOR_CORE
     free = npas.linear_mx_kernel(M, _weights(O, I), dtype=dtype, quantize_x=quantize)
     assert free == kid or free not in TENSOR_CORE            # the same choice where it is among them already
+
+
+def test_queries_ask_about_the_blobs_device(monkeypatch):
+    """The choice counts a device's SMs and a header is read in a stream's order: both of the device that holds the blob."""
+    seen, inside = [], []
+
+    class Device:
+        def __init__(self, t):
+            seen.append(t)
+
+        def __enter__(self):
+            inside.append(True)
+
+        def __exit__(self, *a):
+            inside.pop()
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*a):
+                assert inside, name
+                return 0
+            return call
+
+    monkeypatch.setattr(torch.cuda, "device_of", Device)
+    monkeypatch.setattr(binding, "load", lambda: Library())
+    monkeypatch.setattr(binding, "_stream", lambda: inside[0] and None)
+    w = _weights(1000, 2048)
+    npas.linear_mx_kernel(4, w)
+    npas.linear_mx_workspace(4, w)
+    npas.blob_check(w)
+    assert len(seen) == 3 and all(t is w.data for t in seen)
