@@ -331,13 +331,15 @@ linear_mx_sw_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_con
     if (p.KS > 1) { cluster_arrive(); cluster_wait(); }        // all partial sums are in place; no CTA touches another's memory after this
     else __syncthreads();
     tc_fence_after_sync();
-    if (warp == 1) tmem_dealloc(tmem_base, p.tmem_cols);
-    if (*abort_flag) {
-        // a role gave up: leave time for copies still in flight to land before the CTA retires
+    const bool gave_up = *abort_flag;
+    if (gave_up) {
+        // a role gave up: leave time for copies and MMAs still in flight to land before tensor memory goes back and the CTA retires
         const long long t0 = clock64();
         while (clock64() - t0 < 400000ll) { }
-        return;
+        __syncwarp();
     }
+    if (warp == 1) tmem_dealloc(tmem_base, p.tmem_cols);
+    if (gave_up) return;
     if (p.KS == 1) return;
     const int own = max(0, min(p.cpr, rows - rank * p.cpr));
     for (int i = tid; i < (own + 3) / 4 * kRows; i += kThreads) {
