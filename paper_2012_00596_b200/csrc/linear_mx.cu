@@ -22,6 +22,8 @@ npas_status check_args(const npas_mx_linear_desc *d)
 
 // Up to 16 rows the kernel for few rows quantises the input itself: every CTA its share, again for every 128 outputs.  One launch less
 // (1x2048 -> 1000 6.0 -> 4.2 us of host time); from 32 rows on its CTAs take longer than the launch (32x2048 -> 2048 6.8 us, 6.3 in two).
+// The GPU alone is slower so where the columns are many, since each stage waits for its part of X: 16x4096 -> 8192 14.7 us, 1.8 and 7.2 in two
+// launches; 1x8192 -> 8192 15.7, the product of a blob 9.9.
 bool quantizes_itself(const npas_mx_linear_desc &d) { return d.quantize_x && d.M <= 16; }
 
 npas_mx_linear_desc behind_quantize(npas_mx_linear_desc d)
@@ -214,7 +216,7 @@ npas_status npas_internal_linear_mx(const npas_mx_linear_desc *d, const void *x,
     in.variant = choice.variant;
     if (d->quantize_x && !(kernel == 3 && quantizes_itself(*d))) {
         const npas_mx_desc q = {d->M, d->I, NPAS_BF16};
-        s = quantize_mx_launch(q, x, scratch, st, Launch());
+        s = quantize_mx_launch(q, x, scratch, st);
         if (s != NPAS_OK) return s;
         x = scratch;
         in = behind_quantize(in);

@@ -69,7 +69,7 @@ __device__ __forceinline__ float mx_element_value(uint32_t nibble)
     return __uint_as_float((nibble & 8u) << 28 | (nibble & 7u) << 22) * 0x1p126f;
 }
 
-npas_status quantize_mx_launch(const npas_mx_desc &d, const void *src, void *blob, cudaStream_t st, Launch how);
+npas_status quantize_mx_launch(const npas_mx_desc &d, const void *src, void *blob, cudaStream_t st);
 // (x_pitch: elements from row to row of a 16-bit input, a multiple of 8; a blob has its own)
 bool linear_mx_sw_supported(const npas_mx_linear_desc &d);
 npas_status linear_mx_sw_launch(const npas_mx_linear_desc &d, const void *x, int64_t x_pitch, const void *w, const float *bias, const void *res, void *y,

@@ -264,12 +264,12 @@ Shape shape_of(const npas_mx_desc &d, const MxLayout &L, bool quantize)
     return s;
 }
 template <typename T>
-cudaError_t quantize_any(const npas_mx_desc &d, const Shape &s, const void *src, void *blob, cudaStream_t st, Launch how)
+cudaError_t quantize_any(const npas_mx_desc &d, const Shape &s, const void *src, void *blob, cudaStream_t st)
 {
     const auto kernel = !s.whole ? (s.narrow ? quantize_mx_kernel<T, true, 8, false> : quantize_mx_kernel<T, true, 16, false>)
                       : s.narrow ? (s.parts > 1 ? quantize_mx_kernel<T, true, 8, true> : quantize_mx_kernel<T, false, 8, true>)
                                  : (s.parts > 1 ? quantize_mx_kernel<T, true, 16, true> : quantize_mx_kernel<T, false, 16, true>);
-    return tc::launch_pdl(how, kernel, s.grid, dim3(kThreads), 0, st, (int)d.rows, (int)d.cols, s.parts, static_cast<const T *>(src),
+    return tc::launch_pdl(Launch(), kernel, s.grid, dim3(kThreads), 0, st, (int)d.rows, (int)d.cols, s.parts, static_cast<const T *>(src),
                           static_cast<uint8_t *>(blob));
 }
 template <typename T>
@@ -283,10 +283,10 @@ cudaError_t dequantize_any(const npas_mx_desc &d, const Shape &s, const void *bl
 
 }  // namespace
 
-npas_status quantize_mx_launch(const npas_mx_desc &d, const void *src, void *blob, cudaStream_t st, Launch how)
+npas_status quantize_mx_launch(const npas_mx_desc &d, const void *src, void *blob, cudaStream_t st)
 {
     const Shape s = shape_of(d, mx_layout(d.rows, d.cols), true);
-    const cudaError_t e = d.src_dtype == NPAS_BF16 ? quantize_any<uint16_t>(d, s, src, blob, st, how) : quantize_any<float>(d, s, src, blob, st, how);
+    const cudaError_t e = d.src_dtype == NPAS_BF16 ? quantize_any<uint16_t>(d, s, src, blob, st) : quantize_any<float>(d, s, src, blob, st);
     count_launch();
     return e == cudaSuccess ? launch_status() : NPAS_ERR_CUDA;
 }
@@ -314,7 +314,7 @@ npas_status npas_quantize_mx(const npas_mx_desc *d, const void *src, void *blob,
     if (!aligned16(src) || !aligned16(blob)) return NPAS_ERR_ALIGNMENT;
     if (blob_bytes < mx_layout(d->rows, d->cols).total) return NPAS_ERR_BUFFER_TOO_SMALL;
     if (src == blob) return NPAS_ERR_UNSUPPORTED;
-    return quantize_mx_launch(*d, src, blob, static_cast<cudaStream_t>(stream), Launch());
+    return quantize_mx_launch(*d, src, blob, static_cast<cudaStream_t>(stream));
 }
 
 npas_status npas_dequantize_mx(const npas_mx_desc *d, const void *blob, size_t blob_bytes, int32_t out_dtype, void *out, void *stream)
