@@ -22,7 +22,7 @@ npas_status check_args(const npas_mx_linear_desc *d)
 
 // Up to 16 rows the kernel for few rows quantises the input itself: every CTA its share, again for every 128 outputs.  One launch less
 // (1x2048 -> 1000 6.0 -> 4.2 us of host time); from 32 rows on its CTAs take longer than the launch (32x2048 -> 2048 6.8 us, 6.3 in two).
-// The GPU alone is slower so where the columns are many, since each stage waits for its part of X: 16x4096 -> 8192 14.7 us, 1.8 and 7.2 in two
+// The GPU by itself takes longer that way where the columns are many, since each stage waits for its part of X: 16x4096 -> 8192 14.7 us, 1.8 and 7.2 in two
 // launches; 1x8192 -> 8192 15.7, the product of a blob 9.9.
 bool quantizes_itself(const npas_mx_linear_desc &d) { return d.quantize_x && d.M <= 16; }
 

@@ -8,7 +8,8 @@
 // takes longer than the stage (620).  Copies of both CTAs complete on the leader's barriers, the leader's warp 1 issues the
 // MMAs for both and frees stages and hands over accumulators with multicast commits; both CTAs' epilogues
 // (mx_epi.cuh) read their own 128 lanes; the peer's hand the accumulator back through one arrival with release semantics at cluster
-// scope by its warp 1, as in linear_d2.cu.  Every wait is bounded; a role that gives up raises the abort flag of both CTAs.
+// scope by its warp 1, as in linear_d2.cu.  Every wait is bounded.  A role that waits for the other CTA raises the abort flag of both when it gives
+// up; the others (epilogue, slabs, copies of scales, the relay) raise their own CTA's, and the other one runs into its own limit.
 #include "mx_epi.cuh"
 #include "tc_pair.cuh"
 

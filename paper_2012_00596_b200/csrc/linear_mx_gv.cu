@@ -6,10 +6,11 @@
 // 20.7 us, 11.9 here).  The order of the columns in an MMA is free as long as both operands agree: a thread takes a whole block of 32
 // columns of a row (16 bytes) and one scale, and of X the same 32 columns (64 bytes) of one row, each exactly as it lies in memory.
 // A block of threads has 32 outputs (8a + g, + 32, + 64, + 96 of a tile of scales, whose 16 bytes hold those four rows), a warp every
-// sixteenth tile of 128 columns of them; the warps' sums meet in shared memory and are added in order.  Bound by the SMs' logic pipe (nine of
-// the 17 instructions that widen eight weights, half of them a cycle; 66 % busy where two blocks share an SM) and the two microseconds that a
-// launch, its first loads and its last sums take.  Copies into a ring in shared memory, three shares ahead, cost more instructions than the
-// wait that they save (1x8192 -> 8192 17.2 us).
+// sixteenth tile of 128 columns of them; the warps' sums meet in shared memory and are added in order.  What it takes is no unit's rate: 1x8192 -> 8192 (11.9 us, 5.5 at
+// the copy rate) issues in 57 % of the cycles, the logic pipe (nine of the 17 instructions that widen eight weights) is busy 41 %, memory 30 %; the rest are waits for
+// loads and the two microseconds that a launch, its first loads and its last sums take.  With 16 rows waits for loads come first (16x4096 -> 8192
+// 10.8 us, issue 39 %): every block of 32 outputs reads all of X from L2, 34 MB for 18 MB of weights, and not ahead.  Copies of the weights into a ring in
+// shared memory, three shares ahead, cost more instructions than the wait that they save (1x8192 -> 8192 17.2 us).
 #include "mx_tc.cuh"
 #include "tc_pair.cuh"
 

@@ -9,7 +9,11 @@
 // accumulator.
 // The warps work in groups of eight: with two accumulators a group has every other tile (while one waits for tensor memory or a barrier
 // the other one computes), with one accumulator of 256 columns a block of 128 rows of every tile.  A warp has one quarter of the lanes
-// and 64 of a block's 128 rows; the sums are in its registers, and the accumulator free, before anything else is done with them.
+// and 64 of a block's 128 rows.  When the accumulator is free: through slabs, a warp with one block of a tile hands it back as soon as
+// the sums are in registers; one with both (a 16-bit input and 256 rows; pairs with residuals) has written the first block's slab before it takes the
+// second block's sums; kBoth takes both first.  From registers it is handed back behind the tile's last store.
+// A slab counts as gone when the store of the one after it has been issued, so with NS slabs NS - 1 are being filled: with two, one half of 64
+// outputs after the other.
 #pragma once
 
 #include <type_traits>

@@ -9,8 +9,8 @@
 // which is one 512-byte tile of scales: 16 lanes share a row with eight columns each (one 16-byte load of bf16, one word of
 // nibbles stored), a block's maximum crosses four lanes, eight rows' loads of a thread are in flight together, and the tile of scales
 // is put together in shared memory and leaves in whole sectors.  Maxima and scaling on pairs of bf16: with every element as a float
-// 125 instructions for eight of them bound it (200704x256 57 us, now 21: 94 % of the copy rate; fp32 36.7, 97 %; back 22.3 and
-// 38.6).
+// 125 instructions for eight of them bound it (200704x256 57 us, now 21.2 to 22.5: 89 to 94 % of the copy rate; fp32 37, 97 %; back 22.3, 89 %, and
+// 38.7, 92 %).  Rows off 16-byte boundaries: 2.4 times the instructions, which bound both ways (100000x1003 bf16 issues in 73 % of the cycles, back in 92 %).
 #include <type_traits>
 
 #include "mx_tc.cuh"
